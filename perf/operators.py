@@ -402,15 +402,15 @@ def _own(s):
     if c["op"] == "rope":
         kv.rope(s["x"], s["y"], s["freq"], s["pos"], layout=layout, amplitude=s["amplitude"], inverse=c["inverse"])
         return s["y"]
-    if "workspace" not in s:
-        s["workspace"] = torch.empty(kv.kv_pages_workspace(c["pages"], c["rows"] * c["fan"]), dtype=torch.uint8, device="cuda")
     if c["op"] == "fork":
         kv.kv_free(s["ref"], s["table"], s["kv_len"], s["dst"], c["page"])
-        kv.kv_fork(s["k_cache"], s["v_cache"], s["ref"], s["table"], s["kv_len"], s["src"], s["dst"], s["missing"], workspace=s["workspace"])
+        kv.kv_fork(s["k_cache"], s["v_cache"], s["ref"], s["table"], s["kv_len"], s["src"], s["dst"], s["missing"])
     else:
+        if "workspace" not in s:
+            s["workspace"] = torch.empty(kv.kv_compact_workspace(c["pages"]), dtype=torch.uint8, device="cuda")
         s["table"].copy_(s["table0"])
         s["ref"].copy_(s["ref0"])
-        kv.kv_compact(s["k_cache"], s["v_cache"], s["ref"], s["table"], s["kv_len"], workspace=s["workspace"])
+        kv.kv_compact(s["k_cache"], s["v_cache"], s["ref"], s["table"], s["kv_len"], s["workspace"])
     return s["k_cache"], s["v_cache"], s["table"], s["ref"], s["kv_len"], s["missing"]
 
 

@@ -1,0 +1,404 @@
+// Attention of a packed batch of new tokens over a paged cache (include/kv_cache.h), for gfx950 (MI355X).
+//
+// The rows of a workgroup are (token, query head) pairs that share a key head, so every cached row that comes in serves all of them.
+// The waves of a workgroup work on the same rows and share out the keys: each walks 32 keys at a time with a softmax state of its own
+// (running reference, sum, O), and the states are joined through the LDS at the end.  Nothing waits for another wave before that.  Rows
+// that have few workgroups are also cut along the keys into splits; attn_paged_join joins their results.
+//
+// A wave's keys and values come by direct-to-LDS copies into a ring of its own, one step ahead.  Pages have at least 16
+// tokens, so 16 consecutive keys lie in one page and their address is a scalar.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "launch_once.h"
+#include "paged_launch.h"
+#include "paged_prims.h"
+
+namespace {
+
+// The softmax reference moves only when a row maximum grew by more than this many powers of two.
+constexpr float MOVE_LOG2 = 8.0f;
+constexpr int NW = 4;                           // waves of a workgroup
+
+template <int D, int ES, int QB> struct FewLayout {
+    typedef CachedRows<D, ES, 32> Rows;
+    static constexpr int STAGE = 2 * Rows::BYTES, SLOTS = 2, RING = NW * SLOTS * STAGE;
+    static constexpr int JOIN = NW * (D / 16) * QB * 1024;   // O of every wave
+    static constexpr int SUMS = NW * QB * 16 * 8;            // reference and sum
+    static constexpr int SMEM = (RING > JOIN ? RING : JOIN) + SUMS;
+};
+
+template <int DTYPE, bool C8, int D, int QB>
+__global__ __launch_bounds__(NW * 64)
+void attn_paged_few(PagedArgs a, int tiles)
+{
+    typedef Elem<DTYPE> E;
+    typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
+    typedef typename Layout::Rows Rows;
+    constexpr int KK = D / 32, FB = D / 16, ROWS = QB * 16;
+    constexpr int SUBS = 16 / Rows::PER_PIECE;               // pieces of 16 keys and a line of their rows
+    constexpr int PIECES = 2 * Rows::BYTES / 1024;           // copies of a step
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lc = lane & 15, lg = lane >> 4;
+    const int key_heads = a.heads / a.group;
+    int id = blockIdx.x;
+    const int h = id % key_heads;
+    id /= key_heads;
+    const int sp = id % a.splits;
+    id /= a.splits;
+    const int tile = id % tiles, s = id / tiles;
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    if (tile * ROWS >= seq.n * a.group) return;
+    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal);
+    const int k0 = sp * a.split, k1 = min(keys, k0 + a.split);
+    if (sp > 0 && k0 >= keys) return;
+    const bool whole = keys <= a.split;
+
+    // ---- rows: lane % 16 of each 16-row block
+    s16x8 Qf[QB][KK];
+    int last_key[QB];                           // the last key that the row sees
+    long long o_row[QB];                        // token * heads + head, -1 behind the last row
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = tile * ROWS + qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group;
+        const bool real = tok < seq.n;
+        const int t = seq.q0 + (real ? tok : seq.n - 1);
+        const char* const at = a.q + t * a.q_token + head * a.q_head + lg * 16;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) Qf[qb][kk] = *reinterpret_cast<const s16x8*>(at + kk * 64);
+        last_key[qb] = a.causal ? min(seq.kv - seq.n + tok, keys - 1) : keys - 1;
+        o_row[qb] = real ? (long long)t * a.heads + head : -1;
+    }
+    const int first_last = a.causal ? seq.kv - seq.n + tile * ROWS / a.group : keys - 1;   // what the first row sees
+
+    const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
+    // The reference before the first score: the most negative float whose scaled value is finite.  (-inf would make NaN of rows whose
+    // first keys are hidden.)
+    const float m_none = c > 1.f ? -0x1.fffff0p127f / c : -__FLT_MAX__;
+    f32x4 O[FB][QB];
+    float m_run[QB], neg_mc[QB], L[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m_run[qb] = m_none;
+        neg_mc[qb] = -m_none * c;
+        L[qb] = 0.f;
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) O[fb][qb] = f32x4(0.f);
+    }
+
+    // ---- the wave's steps: 32 keys each, every NW-th of the split's
+    const int blocks = (k1 - k0 + 31) / 32, steps = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
+    const int* const table = a.table + (long long)s * a.table_stride;
+    const int page_mask = (1 << a.page_shift) - 1;
+    int entries = 0;                            // lane 2 i + hf: page of half hf of the i-th step of the current 32
+    auto load_entries = [&](int step) __attribute__((always_inline)) {
+        const int key = min(k0 + ((step + (lane >> 1)) * NW + wave) * 32 + (lane & 1) * 16, keys - 1);
+        entries = table[key >> a.page_shift];
+    };
+    // per-lane source offsets of a copy inside 16 keys: row and (permuted) column
+    unsigned k_off[2][SUBS], v_off[2][SUBS];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            const int r = sub * Rows::PER_PIECE + lane / Rows::COLS, col = lane % Rows::COLS;
+            k_off[hf][sub] = (unsigned)(r * a.token_bytes) + ((col ^ Rows::sw_k(hf * 16 + r)) * 16);
+            v_off[hf][sub] = (unsigned)(r * a.token_bytes) + ((col ^ Rows::sw_v(hf * 16 + r)) * 16);
+        }
+    const unsigned ring = (unsigned)(size_t)(LDS_AS void*)smem + wave * (Layout::SLOTS * Layout::STAGE);
+    const char* const kh = uniform_ptr(a.k + h * a.head_bytes);
+    const char* const vh = uniform_ptr(a.v + h * a.head_bytes);
+    auto issue = [&](int step) __attribute__((always_inline)) -> unsigned {      // the halves of the step that lie in no page
+        const unsigned dst = ring + (step & 1) * Layout::STAGE;
+        const int key = k0 + (step * NW + wave) * 32;
+        unsigned bad = 0;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            int page = __builtin_amdgcn_readlane(entries, (step & 31) * 2 + hf);
+            if ((unsigned)page >= (unsigned)a.pages) {
+                page = 0;
+                bad |= 1u << hf;
+            }
+            const int k_half = key + hf * 16;
+            long long off = page * a.page_bytes;
+            if (k_half + 16 <= keys) {
+                off += (k_half & page_mask) * a.token_bytes;
+#pragma unroll
+                for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+                    for (int g = 0; g < Rows::GROUPS; ++g) {
+                        const unsigned to = dst + g * (32 * Rows::LINE) + (hf * 16 + sub * Rows::PER_PIECE) * Rows::LINE;
+                        dma16(kh + off + g * 128, k_off[hf][sub], to);
+                        dma16(vh + off + g * 128, v_off[hf][sub], to + Rows::BYTES);
+                    }
+            } else {                            // rows behind the last key: that one again (they are masked)
+#pragma unroll
+                for (int sub = 0; sub < SUBS; ++sub) {
+                    const int r = sub * Rows::PER_PIECE + lane / Rows::COLS, col = lane % Rows::COLS;
+                    const unsigned row = (unsigned)((min(k_half + r, keys - 1) & page_mask) * a.token_bytes);
+                    const unsigned ko = row + ((col ^ Rows::sw_k(hf * 16 + r)) * 16), vo = row + ((col ^ Rows::sw_v(hf * 16 + r)) * 16);
+#pragma unroll
+                    for (int g = 0; g < Rows::GROUPS; ++g) {
+                        const unsigned to = dst + g * (32 * Rows::LINE) + (hf * 16 + sub * Rows::PER_PIECE) * Rows::LINE;
+                        dma16(kh + off + g * 128, ko, to);
+                        dma16(vh + off + g * 128, vo, to + Rows::BYTES);
+                    }
+                }
+            }
+        }
+        return bad;
+    };
+
+    if (steps > 0) load_entries(0);
+    // Q is used once here, so that the compiler waits for its loads (and the entries') before the first copy and not for all copies later.
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) asm volatile("" :: "v"(Qf[qb][kk]));
+    unsigned bad = steps > 0 ? issue(0) : 0, bad_next = steps > 1 ? issue(1) : 0;
+
+    for (int step = 0; step < steps; ++step) {
+        if (step + 1 < steps) wait_vmcnt<PIECES>(); else wait_vmcnt<0>();
+        const char* const kt = smem + wave * (Layout::SLOTS * Layout::STAGE) + (step & 1) * Layout::STAGE;
+        const char* const vt = kt + Rows::BYTES;
+        const int key = k0 + (step * NW + wave) * 32;
+        f32x4 S[2][QB];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const s16x8 kf = Rows::template k_operand<DTYPE>(kt, kb, kk, lane);
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) S[kb][qb] = E::mfma16(kf, Qf[qb][kk], kk == 0 ? f32x4(0.f) : S[kb][qb]);
+            }
+        const bool masked = bad != 0 || key + 32 > keys || key + 31 > first_last;
+        if (masked) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                const int lim = (bad >> (lg >> 1)) & 1 ? -1 : last_key[qb];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key + lg * 8 + kb * 4 + i > lim) S[kb][qb][i] = -__builtin_inff();
+            }
+        }
+        u32x4 P[QB];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            float mx = S[0][qb][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) mx = __builtin_fmaxf(mx, S[e / 4][qb][e % 4]);
+            if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(mx, c, neg_mc[qb]) > MOVE_LOG2) != 0) {
+                const float m_old = m_run[qb];
+                m_run[qb] = groups_max(__builtin_fmaxf(mx, m_old));
+                neg_mc[qb] = -m_run[qb] * c;
+                const float alpha = __builtin_amdgcn_exp2f((m_old - m_run[qb]) * c);
+                L[qb] *= alpha;
+#pragma unroll
+                for (int fb = 0; fb < FB; ++fb) O[fb][qb] = O[fb][qb] * alpha;
+            }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    S[kb][qb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[kb][qb][i], c, neg_mc[qb]));
+                    L[qb] += S[kb][qb][i];
+                }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) P[qb][t] = E::pack2(S[t / 2][qb][t % 2 * 2], S[t / 2][qb][t % 2 * 2 + 1]);
+        }
+        // Where some row does not see some key, 0 x NaN would be NaN: there, values that are not finite stay out of the product and
+        // are added key by key to the rows that give them a weight.
+        unsigned found = 0;
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) {
+            u32x4 w = __builtin_bit_cast(u32x4, Rows::template v_operand<DTYPE>(vt, 0, fb, lane));
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const unsigned x = not_finite<DTYPE>(w[t]);
+                    found |= x;
+                    w[t] &= ~x;
+                }
+            }
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) O[fb][qb] = E::mfma16(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, P[qb]), O[fb][qb]);
+        }
+        if (__builtin_amdgcn_ballot_w64(found != 0) != 0) {
+            for (int j = 0; j < 32; ++j) {
+                float p[QB];
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) {
+                    float x = S[0][qb][0];
+#pragma unroll
+                    for (int e = 1; e < 8; ++e) x = (j & 7) == e ? S[e / 4][qb][e % 4] : x;
+                    p[qb] = __shfl(x, (j >> 3) * 16 + lc);
+                }
+#pragma unroll
+                for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = Rows::template v_value<DTYPE>(vt, j, fb * 16 + lg * 4 + i);
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb) O[fb][qb][i] += __builtin_isfinite(x) || p[qb] == 0.f ? 0.f : p[qb] * x;
+                    }
+            }
+        }
+        bad = bad_next;
+        if (step + 2 < steps) {
+            if (((step + 2) & 31) == 0) load_entries(step + 2);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // every read of the slot is done
+            bad_next = issue(step + 2);
+        }
+    }
+
+    // ---- join the waves: each takes a quarter of the features
+    float* const sums = reinterpret_cast<float*>(smem + Layout::SMEM - Layout::SUMS);
+    __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        L[qb] = groups_sum(L[qb]);
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(smem + ((wave * FB + fb) * QB + qb) * 1024 + lane * 16) = O[fb][qb];
+        if (lg == 0) *reinterpret_cast<f32x2*>(sums + ((wave * QB + qb) * 16 + lc) * 2) = f32x2{m_run[qb], L[qb]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        f32x2 ml[NW];
+        float m = m_none, l = 0.f, w[NW];
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            ml[v] = *reinterpret_cast<const f32x2*>(sums + ((v * QB + qb) * 16 + lc) * 2);
+            m = __builtin_fmaxf(m, ml[v][0]);
+        }
+#pragma unroll
+        for (int v = 0; v < NW; ++v) {
+            w[v] = __builtin_amdgcn_exp2f((ml[v][0] - m) * c);
+            l += ml[v][1] * w[v];
+        }
+        const bool real = o_row[qb] >= 0;
+        const int t = real ? (int)(o_row[qb] / a.heads) : 0, head = real ? (int)(o_row[qb] % a.heads) : 0;
+        const long long at = (long long)sp * a.tokens * a.heads + o_row[qb];
+        const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+#pragma unroll
+        for (int f = 0; f < FB / NW; ++f) {
+            const int fb = wave * (FB / NW) + f;
+            f32x4 x = f32x4(0.f);
+#pragma unroll
+            for (int v = 0; v < NW; ++v) x += *reinterpret_cast<const f32x4*>(smem + ((v * FB + fb) * QB + qb) * 1024 + lane * 16) * w[v];
+            if (!real) continue;
+            if (whole) {
+                const u32x2 y = {E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};
+                *reinterpret_cast<u32x2*>(a.o + t * a.o_token + head * a.o_head + (fb * 16 + lg * 4) * 2) = y;
+            } else {
+                *reinterpret_cast<f32x4*>(a.part_o + at * D + fb * 16 + lg * 4) = x;
+            }
+        }
+        if (real && wave == 0 && lg == 0) {
+            if (!whole) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m * c, l};
+            else if (a.lse) a.lse[o_row[qb]] = m * scale + __builtin_logf(l);
+        }
+    }
+}
+
+// ---- the splits of a row joined: a wave a row
+template <int DTYPE, bool C8, int D>
+__global__ __launch_bounds__(256)
+void attn_paged_join(PagedArgs a, int rows)
+{
+    typedef Elem<DTYPE> E;
+    constexpr int PL = D / 64;                  // features per lane
+    const int lane = threadIdx.x & 63;
+    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), all = (long long)a.tokens * a.heads;
+    if (row >= all) return;
+    const int t = (int)(row / a.heads), head = (int)(row % a.heads);
+    const int s = seq_of_token(a.q_start, a.sequences, t, lane);
+    if (s < 0) return;
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    if (t < seq.q0 || t - seq.q0 >= seq.n) return;
+    const int tile = ((t - seq.q0) * a.group + head % a.group) / rows;
+    const int keys = paged_tile_keys(tile, rows, seq.n, a.group, seq.kv, a.causal);
+    if (keys <= a.split) return;
+    const int n = (keys + a.split - 1) / a.split;
+    float m = -__builtin_inff(), l = 0.f, x[PL] = {};
+    for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, a.part_ml[(i * all + row) * 2]);
+    for (int i = 1; i < 64; i *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, i));
+    // (every part has a finite reference, so m is finite)
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (i * all + row) * 2);
+        const float w = __builtin_amdgcn_exp2f(ml[0] - m);
+        l += ml[1] * w;
+#pragma unroll
+        for (int e = 0; e < PL; ++e) x[e] += a.part_o[(i * all + row) * D + lane * PL + e] * w;
+    }
+    const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[head / a.group] : 1.f);
+    char* const dst = a.o + t * a.o_token + head * a.o_head;
+    const unsigned y = E::pack2(x[0] * inv, x[PL - 1] * inv);
+    if constexpr (PL == 2) reinterpret_cast<unsigned*>(dst)[lane] = y;
+    else reinterpret_cast<uint16_t*>(dst)[lane] = (uint16_t)y;
+    if (a.lse && lane == 0) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int DTYPE, bool C8, int D, int QB>
+int launch_few(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
+{
+    typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
+    auto kern = attn_paged_few<DTYPE, C8, D, QB>;
+    static PerDeviceOnce once;
+    if (once.prepare(reinterpret_cast<const void*>(kern), Layout::SMEM) < 0) return -1;
+    PagedArgs arg = a;
+    int tiles = plan.tiles;
+    void* args[] = {&arg, &tiles};
+    const long long grid = (long long)a.sequences * tiles * a.splits * (a.heads / a.group);
+    return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, Layout::SMEM, stream) == hipSuccess ? 0 : -1;
+}
+
+template <int DTYPE, bool C8, int D>
+int launch_all(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
+{
+    int rc;
+    if (plan.rows == 16) rc = launch_few<DTYPE, C8, D, 1>(a, plan, stream);
+    else if (plan.rows == 32) rc = launch_few<DTYPE, C8, D, 2>(a, plan, stream);
+    else rc = launch_few<DTYPE, C8, D, 4>(a, plan, stream);
+    if (rc != 0 || a.splits == 1) return rc;
+    PagedArgs arg = a;
+    int rows = plan.rows;
+    void* args[] = {&arg, &rows};
+    const unsigned grid = (unsigned)(((long long)a.tokens * a.heads + 3) / 4);
+    return hipLaunchKernel(reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D>), dim3(grid), dim3(256), args, 0, stream) == hipSuccess ? 0 : -1;
+}
+
+}  // namespace
+
+PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes)
+{
+    (void)tokens; (void)d; (void)cache_bytes;
+    const long long most = (long long)max_q * (heads / key_heads);
+    PagedPlan p;
+    p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    p.tiles = (int)((most + p.rows - 1) / p.rows);
+    // Keys per split: so many that about 8 workgroups a compute unit come out if all sequences are long, 512 at least.
+    const long long units = (long long)sequences * p.tiles * key_heads;
+    long long split = (units * max_kv / (8 * 256) + 127) / 128 * 128;
+    if (split < 512) split = 512;
+    if (split > max_kv) split = (max_kv + 127) / 128 * 128;
+    p.split = (int)split;
+    p.splits = (int)((max_kv + split - 1) / split);
+    return p;
+}
+
+int attn_paged_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream)
+{
+    const hipStream_t st = (hipStream_t)stream;
+    if (cache_dtype == KV_E4M3) {
+        if (dtype == 0) return d == 128 ? launch_all<0, true, 128>(a, plan, st) : launch_all<0, true, 64>(a, plan, st);
+        return d == 128 ? launch_all<1, true, 128>(a, plan, st) : launch_all<1, true, 64>(a, plan, st);
+    }
+    if (dtype == 0) return d == 128 ? launch_all<0, false, 128>(a, plan, st) : launch_all<0, false, 64>(a, plan, st);
+    return d == 128 ? launch_all<1, false, 128>(a, plan, st) : launch_all<1, false, 64>(a, plan, st);
+}

@@ -1,0 +1,86 @@
+// Internal seam between the host side of include/kv_cache.h (kv_api.cpp) and its kernels.
+#pragma once
+
+#include "kv_cache.h"
+
+#if defined(__HIPCC__)
+#define PAGED_HD __host__ __device__
+#else
+#define PAGED_HD
+#endif
+
+// What the attention kernels of one call share.
+struct PagedArgs {
+    const char *k, *v;
+    const float *k_scale, *v_scale;
+    long long page_bytes, head_bytes, token_bytes;          // strides of the cache
+    const int *q_start, *kv_len, *table;
+    const char* q;
+    char* o;
+    float* lse;
+    long long q_token, q_head, o_token, o_head;              // strides, bytes
+    float *part_o, *part_ml;                                 // partial results: [split][token * heads + head][d], [..][2]
+    int sequences, tokens, table_stride, max_q, max_kv, pages, page_shift;
+    int heads, group;                                        // query heads, and how many share a key head
+    int causal, split, splits;                               // keys per split (a multiple of 128), splits of the longest sequence
+    float scale;
+};
+
+// How a call is laid out (chosen by its sizes alone, so that the workspace is known beforehand).
+struct PagedPlan {
+    int rows;                                                // query rows (tokens x heads of a group) per workgroup
+    int tiles;                                               // row tiles of the sequence with the most new tokens
+    int split, splits;
+};
+PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes);
+
+// Row tiles as they are cut from a sequence: tile t has the rows t * rows ... of the n * group rows (token-major) of its n new tokens.
+// Keys that its rows may see, and in how many splits.
+PAGED_HD inline int paged_tile_keys(int tile, int rows, int n, int group, int kv, int causal)
+{
+    if (!causal) return kv;
+    const int last = (tile + 1) * rows - 1, token = last / group;
+    const int end = kv - n + (token < n ? token : n - 1) + 1;
+    return end < 0 ? 0 : end;
+}
+
+// Enqueue for validated arguments: 0, or -1 if HIP refused a launch.
+int attn_paged_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream);
+
+struct RopeArgs {
+    const char* x;
+    char* y;
+    const int* pos;
+    const double* freq;
+    long long x_batch, x_head, x_token, y_batch, y_head, y_token, pos_stride;    // bytes (pos: entries)
+    int batches, heads, tokens, d, rot, layout;
+    float cos_factor, sin_factor;                            // amplitude, and amplitude with the sign of the direction
+};
+int rope_launch(const RopeArgs& a, int dtype, void* stream);
+
+struct AppendArgs {
+    char *k_cache, *v_cache;
+    const float *k_scale, *v_scale;
+    long long page_bytes, head_bytes, token_bytes;
+    const int *q_start, *kv_len, *table;
+    const char *k, *v, *q;
+    char* q_out;
+    const double* freq;
+    long long k_token, k_head, v_token, v_head, q_token, q_head, o_token, o_head;
+    int sequences, tokens, table_stride, max_q, max_kv, pages, page_shift;
+    int heads, key_heads, d, rot, layout;                    // heads 0: no Q
+    float amplitude;
+};
+int kv_append_launch(const AppendArgs& a, int dtype, int cache_dtype, void* stream);
+
+// Contents of pages: rows of row_bytes, [layers][page][heads][tokens] by strides in bytes.
+struct PageCopy {
+    char *k, *v;
+    long long layer, page, head, token;
+    int layers, pages, heads, page_size, row_bytes;
+};
+int kv_reserve_launch(const kv_book& b, const int* list, const int* new_len, int n, int* missing, void* stream);
+int kv_free_launch(const kv_book& b, const int* list, int n, void* stream);
+int kv_fork_launch(const PageCopy& c, const kv_book& b, const int* src, const int* dst, int n, int* missing, void* stream);
+int kv_compact_launch(const PageCopy& c, const kv_book& b, int* workspace, void* stream);
+int kv_copy_pages_launch(const PageCopy& c, const int* src, const int* dst, int n, void* stream);

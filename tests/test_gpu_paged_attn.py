@@ -1,0 +1,230 @@
+"""Attention over a paged cache against its definition in 64 bits.  Everything in a cache that no token was written to is NaN."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.paged_util import LSE_FILL, O_FILL, Batch, check, workspace_for
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def kv():
+    from paper_2510_14719_amd import kv_cache
+    return kv_cache
+
+
+def call(kv, b, dev, causal=True, lse=True, workspace="fresh", max_kv=None, **kw):
+    args = dict(dev)
+    if workspace == "fresh":
+        workspace = workspace_for(kv, args["q"], args["k_cache"], len(b.lens), b.max_q, max_kv or b.max_kv)
+    kv.attn_paged(args["q"], args["k_cache"], args["v_cache"], args["q_start"], args["kv_len"], args["table"], args["o"], args["lse"] if lse else None, b.max_q,
+                  max_kv or b.max_kv, 1 / math.sqrt(b.d), causal, workspace=workspace, **args["scales"], **kw)
+
+
+def run(kv, b, causal=True, what="", **kw):
+    dev = b.cuda()
+    call(kv, b, dev, causal, **kw)
+    torch.cuda.synchronize()
+    check(dev["o"], dev["lse"], b.reference(1 / math.sqrt(b.d), causal), what)
+    return dev
+
+
+STEP = [(1, 1), (1, 2), (1, 15), (1, 16), (1, 17), (1, 31), (1, 33), (1, 127), (1, 128), (1, 129), (1, 300)]
+FEW = [(3, 3), (2, 40), (5, 5), (1, 1), (7, 200), (4, 64), (6, 161)]
+MANY = [(33, 33), (1, 70), (70, 133), (100, 100), (17, 257)]
+CASES = [
+    # lens, heads, key heads, d, tokens, cache, page, order, causal
+    (STEP, 2, 2, 64, "fp16", "fp16", 16, "head", True), (STEP, 8, 2, 128, "bf16", "bf16", 16, "token", True),
+    (STEP, 8, 1, 128, "fp16", "e4m3", 64, "head", True), (STEP, 5, 1, 64, "bf16", "e4m3", 32, "token", True),
+    (STEP, 16, 1, 128, "bf16", "bf16", 128, "head", False), (STEP, 17, 1, 64, "fp16", "fp16", 16, "head", True),
+    (STEP, 48, 1, 128, "fp16", "fp16", 16, "token", True), (STEP, 33, 1, 64, "bf16", "e4m3", 16, "head", True),
+    (FEW, 4, 4, 128, "fp16", "fp16", 16, "head", True), (FEW, 6, 2, 64, "bf16", "bf16", 32, "head", True),
+    (FEW, 8, 2, 128, "bf16", "e4m3", 16, "token", True), (FEW, 8, 1, 64, "fp16", "fp16", 256, "head", False),
+    (FEW, 7, 1, 128, "fp16", "e4m3", 32, "head", True),
+    (MANY, 2, 2, 128, "bf16", "bf16", 16, "head", True), (MANY, 4, 2, 64, "fp16", "fp16", 64, "token", True),
+    (MANY, 3, 1, 128, "fp16", "e4m3", 16, "head", True), (MANY, 5, 1, 128, "bf16", "bf16", 32, "token", False),
+    (MANY, 6, 2, 64, "bf16", "e4m3", 32, "head", False), (MANY, 8, 1, 64, "fp16", "fp16", 16, "head", True),
+]
+
+
+@pytest.mark.parametrize("lens,H,Hk,d,dtype,cache,page,order,causal", CASES)
+def test_against_the_definition(kv, lens, H, Hk, d, dtype, cache, page, order, causal):
+    run(kv, Batch(lens, H, Hk, d, dtype, cache, page, order, pad=3), causal)
+
+
+@pytest.mark.parametrize("d,dtype,cache", [(64, "fp16", "fp16"), (128, "bf16", "bf16"), (128, "fp16", "e4m3"), (64, "bf16", "e4m3")])
+@pytest.mark.parametrize("n", [1, 5, 40])
+def test_long_rows_are_split_and_joined(kv, d, dtype, cache, n):
+    b = Batch([(n, 2309), (n, 700), (1, 5), (n, 4097)], 4, 2, d, dtype, cache, 16, peaky=True)
+    assert kv.attn_paged_workspace(b.q.cuda(), b.k_cache.cuda(), 4, b.max_q, b.max_kv) > 0
+    run(kv, b)
+
+
+@pytest.mark.parametrize("dtype,cache", [("fp16", "fp16"), ("bf16", "bf16"), ("bf16", "e4m3")])
+def test_a_long_chunk(kv, dtype, cache):
+    run(kv, Batch([(300, 1111)], 4, 2, 128, dtype, cache, 32, peaky=True), what="chunk of 300")
+    run(kv, Batch([(513, 513), (2, 600)], 2, 1, 64, dtype, cache, 64), what="chunk of 513")
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_rows_that_see_nothing(kv, cache):
+    # sequences without new tokens, without keys, with more new tokens than keys, in pages that are none
+    lens = [(0, 0), (1, 0), (0, 30), (5, 2), (40, 7), (1, 20), (3, 100), (0, 0)]
+    holes = [(5, 0), (5, 1), (6, 0), (6, 1), (6, 2), (6, 3), (6, 4), (6, 5)]
+    for causal in (True, False):
+        dev = run(kv, Batch(lens, 4, 2, 64, "bf16", cache, 16, holes=holes, pad=1), causal)
+        assert bool((dev["lse"][:1] == -math.inf).all())
+
+
+@pytest.mark.parametrize("n", [1, 3, 50])
+def test_pages_that_are_none(kv, n):
+    run(kv, Batch([(n, 1000), (n, 130)], 4, 1, 128, "fp16", "fp16", 16, holes=[(0, 3), (0, 30), (0, 31), (0, 62), (1, 0), (1, 8)]))
+    run(kv, Batch([(n, 1000)], 4, 1, 64, "bf16", "e4m3", 32, holes=[(0, 0), (0, 31)]), causal=False)
+
+
+@pytest.mark.parametrize("cache,value", [("fp16", math.inf), ("fp16", -math.inf), ("fp16", math.nan), ("e4m3", math.nan)])
+@pytest.mark.parametrize("n,G", [(2, 1), (6, 4), (40, 2)])
+def test_what_a_row_does_not_see_does_not_touch_it(kv, cache, value, n, G):
+    """The newest token's K is NaN and its V not finite: only its own rows notice.  The one before has a V that is not finite: its own and later rows."""
+    b = Batch([(n, 100), (n, n), (n, 64)], 2 * G, 2, 64, "fp16", cache, 16)
+    for s, (_, m) in enumerate(b.lens):
+        b.v[s][m - 1, :, 5] = value
+        b.v[s][m - 2, 1, 63] = value
+        if s == 0:
+            b.k[s][m - 1, 0, 3] = math.nan
+        b.put(s, m - 1)
+        b.put(s, m - 2)
+    with np.errstate(invalid="ignore"):
+        run(kv, b)
+
+
+def test_bounds_that_are_not_tight_and_no_lse(kv):
+    b = Batch(FEW, 4, 2, 128, "bf16", "bf16", 16, width=200)
+    want = run(kv, b)
+    dev = b.cuda()
+    b.max_q = 31
+    call(kv, b, dev, lse=False, max_kv=3200)
+    torch.cuda.synchronize()
+    check(dev["o"], want["lse"], b.reference(1 / math.sqrt(128), True))
+    assert bool((dev["lse"] == LSE_FILL).all())
+
+
+def test_lengths_outside_their_bounds_are_brought_into_them(kv):
+    """Nothing is read or written out of range, whatever the arrays hold; sequences that are in order come out right."""
+    b = Batch([(2, 40), (3, 50), (1, 9)], 4, 2, 64, "fp16", "fp16", 16, pad=4)
+    dev = b.cuda()
+    ref = b.reference(1 / 8, True)
+    dev["kv_len"].copy_(torch.tensor([40, 2 ** 31 - 1, 9], dtype=torch.int32))      # (cut to max_kv; its last table entries are no pages)
+    dev["table"][1, 3:] = -1
+    call(kv, b, dev)
+    torch.cuda.synchronize()
+    rows = [0, 1, 5, 6, 7, 8, 9]
+    check(dev["o"][rows], dev["lse"][rows], [x[rows] for x in ref])
+    for starts, lens in (([-5, 2, 2 ** 31 - 1, -9], [40, -3, 9]), ([0, 9, 3, 6], [40, 50, 9]), ([2 ** 31 - 1] * 4, [0, 0, 0])):
+        dev["q_start"].copy_(torch.tensor(starts, dtype=torch.int32))
+        dev["kv_len"].copy_(torch.tensor(lens, dtype=torch.int32))
+        call(kv, b, dev)
+        torch.cuda.synchronize()
+
+
+def test_strides(kv):
+    """Q and O as slices of wider arrays in either order of heads and tokens, tables wider than their rows, K and V side by side in one pool."""
+    b = Batch(FEW, 4, 2, 64, "fp16", "fp16", 16, pad=2)
+    want = run(kv, b)
+    dev = b.cuda()
+    T = b.tokens
+    wide = torch.full((T, 9, 64), 7.0, dtype=torch.float16, device="cuda")
+    wide[:, 1:5] = dev["q"]
+    dev["q"] = wide[:, 1:5]
+    out = torch.full((6, T + 5, 64), O_FILL, dtype=torch.float16, device="cuda")
+    dev["o"] = out[1:5, 2:T + 2].transpose(0, 1)
+    pool = torch.full((b.k_cache.shape[0], 2, 3, 16, 80), float("nan"), dtype=torch.float16, device="cuda")
+    pool[:, 0, :2, :, :64], pool[:, 1, :2, :, :64] = dev["k_cache"], dev["v_cache"]
+    dev["k_cache"], dev["v_cache"] = pool[:, 0, :2, :, :64], pool[:, 1, :2, :, :64]
+    table = torch.full((len(FEW), 50), 2 ** 30, dtype=torch.int32, device="cuda")
+    table[:, :dev["table"].shape[1]] = dev["table"]
+    dev["table"] = table[:, :dev["table"].shape[1]]
+    call(kv, b, dev)
+    torch.cuda.synchronize()
+    assert torch.equal(dev["o"], want["o"]) and torch.equal(dev["lse"], want["lse"])
+    assert bool((out[0] == O_FILL).all()) and bool((out[5] == O_FILL).all()) and bool((out[:, :2] == O_FILL).all()) and bool((out[:, T + 2:] == O_FILL).all())
+
+
+@pytest.mark.parametrize("n,dtype,cache", [(1, "bf16", "bf16"), (90, "fp16", "e4m3")])
+def test_offsets_beyond_32_bits(kv, n, dtype, cache):
+    """The last pages of a cache of 6 GiB each for K and V."""
+    b = Batch([(n, 530), (n, 100)], 4, 2, 128, dtype, cache, 64)
+    dev = b.cuda()
+    want = {k: v.clone() if torch.is_tensor(v) else v for k, v in dev.items()}
+    call(kv, b, want)
+    size = dev["k_cache"].element_size()
+    small = b.k_cache.shape[0]
+    pages = (6 << 30) // (2 * 64 * 128 * size)
+    for name in ("k_cache", "v_cache"):
+        big = torch.empty((pages, 2, 64, 128), dtype=dev[name].dtype, device="cuda")
+        big[pages - small:].view(torch.uint8).copy_(dev[name].view(torch.uint8))
+        dev[name] = big
+    dev["table"].add_(pages - small)
+    call(kv, b, dev)
+    torch.cuda.synchronize()
+    assert torch.equal(dev["o"], want["o"]) and torch.equal(dev["lse"], want["lse"])
+
+
+def test_other_streams_and_graphs(kv):
+    """Two captured calls share a workspace and are replayed by turns while lengths change on the device; every replay equals the eager call."""
+    b = Batch([(2, 2000), (2, 900), (2, 77)], 4, 2, 64, "bf16", "bf16", 16, seed=5)
+    first, second = b.cuda(), b.cuda()
+    second["q"].mul_(-1)
+    n = kv.attn_paged_workspace(first["q"], first["k_cache"], 3, 2, 2000)
+    assert n > 0
+    ws = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    call(kv, b, first, workspace=ws, stream=side)
+    side.synchronize()
+    graphs = []
+    for dev in (first, second):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(kv, b, dev, workspace=ws)
+        graphs.append(g)
+    for lens in ([2000, 900, 77], [1999, 2, 40], [17, 900, 3], [2000, 900, 77]):
+        for dev, g in zip((first, second), graphs):
+            dev["kv_len"].copy_(torch.tensor(lens, dtype=torch.int32))
+            dev["o"].fill_(float("nan"))
+            g.replay()
+        torch.cuda.synchronize()
+        for dev in (first, second):
+            eager = {k: v.clone() if torch.is_tensor(v) else v for k, v in dev.items()}
+            eager["o"].fill_(3.0)
+            call(kv, b, eager)
+            torch.cuda.synchronize()
+            assert torch.equal(eager["o"], dev["o"]) and torch.equal(eager["lse"], dev["lse"])
+            assert not dev["o"].isnan().any()
+
+
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (64, "fp16")])
+def test_beside_the_contiguous_attention(kv, d, dtype):
+    """A prompt read whole, and in chunks, gives what attn_fwd gives for it: both are within their bounds of the same definition."""
+    from paper_2510_14719_amd import binding
+    N = 333
+    b = Batch([(N, N)], 3, 3, d, dtype, dtype, 16, seed=9)
+    ref = b.reference(1 / math.sqrt(d), True)
+    dev = run(kv, b)
+    q, k, v = (x.transpose(0, 1).contiguous()[None].cuda() for x in (b.q, b.k[0], b.v[0]))
+    o, lse = torch.empty_like(q), torch.empty((1, 3, N), device="cuda")
+    binding.attn_fwd(q, k, v, o, lse, 1, 3, N, d, 1 / math.sqrt(d), True)
+    torch.cuda.synchronize()
+    err = (o[0].transpose(0, 1).double() - dev["o"].double()).abs().cpu().numpy()
+    assert (err <= 2 * ref[2] + 2 * 2.0 ** -8 * np.abs(ref[0])).all()              # (attn_fwd normalises by the sum of the rounded weights: another u)
+    for at in range(0, N, 100):
+        end = min(N, at + 100)
+        out, l2 = torch.empty_like(dev["o"][at:end]), torch.empty_like(dev["lse"][at:end])
+        kv.attn_paged(dev["q"][at:end], dev["k_cache"], dev["v_cache"], torch.tensor([0, end - at], dtype=torch.int32, device="cuda"),
+                      torch.tensor([end], dtype=torch.int32, device="cuda"), dev["table"], out, l2, end - at, end, 1 / math.sqrt(d),
+                      workspace=workspace_for(kv, dev["q"][at:end], dev["k_cache"], 1, end - at, end))
+        torch.cuda.synchronize()
+        check(out, l2, [x[at:end] for x in ref], "tokens from %d" % at)

@@ -1,0 +1,444 @@
+// Attention of chunks of new tokens over a paged cache (include/kv_cache.h), many query rows at a time, for gfx950 (MI355X).
+//
+// A workgroup takes 256 rows, (token, query head) pairs that share a key head, 32 to a wave, and walks the keys in tiles of 64.  Its two
+// groups of four waves (one wave of each on a SIMD) run half a period apart:
+//     group A after barrier j:  [U_{j-1}, T_j] on the matrix cores, then C_j on the vector ALU
+//     group B after barrier j:  C_j on the vector ALU, then [U_j, T_{j+1}] on the matrix cores
+// with T = Q K^T, C = softmax against a running reference, U = P V of a tile, so that one wave of a SIMD streams MFMAs while the other does its softmax.
+// Keys and values come by direct-to-LDS copies into a ring of four stages (K tile s + 1 and V tile s are stage s), two tiles ahead; a page has at
+// least 16 tokens, so the 8 or 16 rows of a copy lie in one page.
+//
+// Tiles that some row sees only in part (the diagonal, the end, missing pages) come last or are rare: a loop of their own masks the scores and
+// keeps values that are not finite out of the product (see careful_u).
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "launch_once.h"
+#include "paged_launch.h"
+#include "paged_prims.h"
+
+namespace {
+
+constexpr float MOVE_LOG2 = 8.0f;               // the reference moves when a maximum grew by more than this many powers of two
+constexpr int NW = 8, BM = PAGED_CHUNK_ROWS, BN = 64, STAGES = 4, QB = 2, KB = BN / 16;
+constexpr int AHEAD = 2;                        // LDS operands requested ahead of their MFMA
+
+template <int DTYPE, bool C8, int D>
+__global__ __launch_bounds__(NW * 64)
+void attn_paged_chunk(PagedArgs a)
+{
+    typedef Elem<DTYPE> E;
+    typedef CachedRows<D, C8 ? 1 : 2, BN> Rows;
+    constexpr int KK = D / 32, FB = D / 16, STAGE = 2 * Rows::BYTES;
+    constexpr int PIECES = Rows::BYTES / 1024;               // copies of a K or V tile
+    constexpr int PPW = 2 * PIECES / NW;                     // copies of a stage that a wave issues: 4 (K, K, V, V), 2 (K, V) or 1
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lc = lane & 15, lg = lane >> 4;
+    const bool group_b = wave >= NW / 2;
+
+    // ---- which rows: tiles of the sequences that are long enough, numbered through; long ones (late tokens) first inside a sequence
+    const int key_heads = a.heads / a.group;
+    int id = blockIdx.x;
+    const int h = id % key_heads;
+    id /= key_heads;
+    const int sp = id % a.chunk_splits;
+    int left = id / a.chunk_splits, s = -1, tile = 0;
+    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+        int mine = 0;
+        if (s0 + lane < a.sequences) {
+            const int rows = seq_range(a.q_start, a.kv_len, s0 + lane, a.tokens, a.max_q, a.max_kv).n * a.group;
+            mine = rows > a.few_rows ? (rows + BM - 1) / BM : 0;
+        }
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(sum, d);
+            if (lane >= d) sum += x;
+        }
+        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(sum > left);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond);
+            s = s0 + at;
+            tile = __builtin_amdgcn_readlane(sum, at) - 1 - left;        // (from the last to the first)
+            break;
+        }
+        left -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    if (s < 0) return;
+    s = __builtin_amdgcn_readfirstlane(s);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    const int keys = __builtin_amdgcn_readfirstlane(paged_tile_keys(tile, BM, seq.n, a.group, seq.kv, a.causal));
+    const int k0 = sp * a.chunk_split, k1 = min(keys, k0 + a.chunk_split);
+    if (sp > 0 && k0 >= keys) return;
+    const bool whole = keys <= a.chunk_split;
+
+    // ---- rows of this wave, lane % 16 of each 16-row block
+    const int wq0 = tile * BM + wave * (QB * 16);
+    s16x8 Qf[QB][KK];
+    int last_key[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = wq0 + qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group;
+        const bool real = tok < seq.n;
+        const int t = seq.q0 + (real ? tok : seq.n - 1);
+        const char* const at = a.q + t * a.q_token + head * a.q_head + lg * 16;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) Qf[qb][kk] = *reinterpret_cast<const s16x8*>(at + kk * 64);
+        last_key[qb] = a.causal ? min(seq.kv - seq.n + tok, keys - 1) : keys - 1;
+    }
+    // keys of the split that any row of this wave sees, and those that all of them see, in tiles
+    int nt = (k1 - k0 + BN - 1) / BN, nt_w, nt_full;
+    {
+        const int first_tok = wq0 / a.group, last_tok = min((wq0 + QB * 16 - 1) / a.group, seq.n - 1);
+        const int w_end = first_tok >= seq.n ? 0 : a.causal ? min(k1, seq.kv - seq.n + last_tok + 1) : k1;
+        const int w_all = a.causal ? min(k1, seq.kv - seq.n + first_tok + 1) : k1;
+        nt = max(nt, 0);
+        nt_w = w_end > k0 ? (w_end - k0 + BN - 1) / BN : 0;
+        nt_full = w_all > k0 ? min((w_all - k0) / BN, nt_w) : 0;
+    }
+    nt = __builtin_amdgcn_readfirstlane(nt);
+    nt_w = __builtin_amdgcn_readfirstlane(nt_w);
+    nt_full = __builtin_amdgcn_readfirstlane(nt_full);
+
+    const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
+    const float m_none = c > 1.f ? -0x1.fffff0p127f / c : -__FLT_MAX__;  // (the most negative float whose scaled value is finite)
+
+    // ---- copies.  A wave's pieces are rows of one 16-key block of the tile and one 128-byte group of a row.
+    const bool copies_k = PPW > 1 || wave < NW / 2, copies_v = PPW > 1 || wave >= NW / 2;
+    const int block = PPW == 2 ? wave >> 1 : wave & 3;       // 16-key block
+    const int group = PPW == 4 ? wave >> 2 : 0;
+    constexpr int SUBS = PPW == 4 ? 2 : 1;                   // pieces of K (and of V)
+    const int sub0 = PPW == 2 ? wave & 1 : 0;
+    unsigned k_off[SUBS], v_off[SUBS];
+    int piece_row[SUBS];                                     // of the lane, inside the 16 keys
+#pragma unroll
+    for (int i = 0; i < SUBS; ++i) {
+        const int r = (sub0 + i) * Rows::PER_PIECE + lane / Rows::COLS, col = lane % Rows::COLS;
+        piece_row[i] = r;
+        k_off[i] = (unsigned)((col ^ Rows::sw_k(block * 16 + r)) * 16 + group * 128);
+        v_off[i] = (unsigned)((col ^ Rows::sw_v(block * 16 + r)) * 16 + group * 128);
+    }
+    const unsigned lds = (unsigned)(size_t)(LDS_AS void*)smem;
+    const int to0 = group * (BN * Rows::LINE) + (block * 16 + sub0 * Rows::PER_PIECE) * Rows::LINE;
+    const char* const kh = uniform_ptr(a.k + h * a.head_bytes);
+    const char* const vh = uniform_ptr(a.v + h * a.head_bytes);
+    const int* const table = a.table + (long long)s * a.table_stride;
+    const int page_mask = (1 << a.page_shift) - 1, token_bytes = (int)a.token_bytes;
+    int entries = 0;                            // lane i: page of this wave's block of tile i of the current 64
+    bool any_bad = false;                       // a page of the tiles so far is none
+    int page_k = 0, page_v = 0;
+    auto load_entries = [&](int t0) __attribute__((always_inline)) {
+        const int key = k0 + (t0 + lane) * BN;
+        bool bad = false;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) bad |= (unsigned)table[min(key + b * 16, keys - 1) >> a.page_shift] >= (unsigned)a.pages;
+        entries = table[min(key + block * 16, keys - 1) >> a.page_shift];
+        any_bad |= __builtin_amdgcn_ballot_w64(bad) != 0;
+    };
+    auto copy_tile = [&](const char* base, int page, int t, const unsigned (&off)[SUBS], unsigned dst) __attribute__((always_inline)) {
+        const int key = k0 + t * BN + block * 16;
+        const char* const at = base + page * a.page_bytes;
+        if (key + 16 <= keys) {
+            const char* const from = at + (key & page_mask) * token_bytes;
+#pragma unroll
+            for (int i = 0; i < SUBS; ++i) dma16(from, off[i] + piece_row[i] * token_bytes, dst + i * (Rows::PER_PIECE * Rows::LINE));
+        } else {                                // rows behind the last key: that one again (they are masked, or never read)
+#pragma unroll
+            for (int i = 0; i < SUBS; ++i)
+                dma16(at, off[i] + (min(key + piece_row[i], keys - 1) & page_mask) * token_bytes, dst + i * (Rows::PER_PIECE * Rows::LINE));
+        }
+    };
+    auto issue_stage = [&](int st) __attribute__((always_inline)) {      // in order, from -1 on
+        const unsigned dst = lds + ((st + STAGES) % STAGES) * STAGE + to0;
+        const int t = st + 1;
+        if (t < nt) {
+            if ((t & 63) == 0) load_entries(t);
+            const int page = __builtin_amdgcn_readlane(entries, t & 63);
+            page_v = page_k;
+            page_k = (unsigned)page < (unsigned)a.pages ? page : 0;
+        } else {
+            page_v = page_k;
+        }
+        // (behind the last tile, and before the first, something is copied all the same: the waits count copies)
+        if (copies_k) copy_tile(kh, page_k, min(t, nt - 1), k_off, dst);
+        if (copies_v) copy_tile(vh, t == 0 ? page_k : page_v, max(st, 0), v_off, dst + Rows::BYTES);
+    };
+    auto wait_stage = [&](int j) __attribute__((always_inline)) {
+        if (j + 1 < nt) wait_vmcnt<PPW>(); else wait_vmcnt<0>();
+        __builtin_amdgcn_s_barrier();
+    };
+    auto stage_ptr = [&](int st) __attribute__((always_inline)) -> const char* { return smem + ((st + STAGES) % STAGES) * STAGE; };
+
+    f32x4 O[FB][QB], S[KB][QB];
+    u32x4 pw[KB / 2][QB];
+    float m_run[QB], neg_mc[QB], L[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m_run[qb] = m_none;
+        neg_mc[qb] = -m_none * c;
+        L[qb] = 0.f;
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) O[fb][qb] = f32x4(0.f);
+    }
+
+    // ---- U and / or T on one stage as one stream of MFMAs, operands requested AHEAD MFMAs before their use
+    auto burst = [&](auto do_u, auto do_t, const char* st) __attribute__((always_inline)) {
+        constexpr int NU = decltype(do_u)::value ? KB / 2 * FB : 0, NT = decltype(do_t)::value ? KB * KK : 0, NF = NU + NT;
+        s16x8 fr[NF];
+        auto fetch = [&](int f) __attribute__((always_inline)) {
+            if (f < NU) fr[f] = Rows::template v_operand<DTYPE>(st + Rows::BYTES, f / FB, f % FB, lane);
+            else fr[f] = Rows::template k_operand<DTYPE>(st, (f - NU) % KB, (f - NU) / KB, lane);
+        };
+#pragma unroll
+        for (int f = 0; f < AHEAD; ++f) fetch(f);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            if (f + AHEAD < NF) fetch(f + AHEAD);
+            if (f < NU) {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) O[f % FB][qb] = E::mfma16(fr[f], __builtin_bit_cast(s16x8, pw[f / FB][qb]), O[f % FB][qb]);
+            } else {
+                const int kb = (f - NU) % KB, kk = (f - NU) / KB;
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) S[kb][qb] = E::mfma16(fr[f], Qf[qb][kk], kk == 0 ? f32x4(0.f) : S[kb][qb]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // ---- U of a tile that some row sees in part: 0 x NaN would be NaN, so values that are not finite stay out of the product and are
+    // added key by key to the rows that give them a weight.
+    auto careful_u = [&](const char* st) __attribute__((always_inline)) {
+        const char* const vt = st + Rows::BYTES;
+        unsigned found = 0;
+#pragma unroll
+        for (int kc = 0; kc < KB / 2; ++kc)
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb) {
+                u32x4 w = __builtin_bit_cast(u32x4, Rows::template v_operand<DTYPE>(vt, kc, fb, lane));
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const unsigned x = not_finite<DTYPE>(w[t]);
+                    found |= x;
+                    w[t] &= ~x;
+                }
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) O[fb][qb] = E::mfma16(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, pw[kc][qb]), O[fb][qb]);
+            }
+        if (__builtin_amdgcn_ballot_w64(found != 0) == 0) return;
+        for (int j = 0; j < BN; ++j) {
+            float p[QB];
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                unsigned x = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x = (j >> 3 & 4) + (j >> 1 & 3) == e ? pw[e / 4][qb][e % 4] : x;
+                x = __shfl(x, (j >> 3 & 3) * 16 + lc);
+                p[qb] = to_float<DTYPE>((uint16_t)(j & 1 ? x >> 16 : x));
+            }
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = Rows::template v_value<DTYPE>(vt, j, fb * 16 + lg * 4 + i);
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) O[fb][qb][i] += __builtin_isfinite(x) || p[qb] == 0.f ? 0.f : p[qb] * x;
+                }
+        }
+    };
+
+    // ---- C of tile j: S into pw
+    auto softmax_tile = [&](int j, auto masked) __attribute__((always_inline)) {
+        if (decltype(masked)::value) {
+            const int key0 = k0 + j * BN;
+            unsigned bad = 0;                   // 16-key blocks in no page
+            if (any_bad) {
+#pragma unroll
+                for (int b = 0; b < KB; ++b)
+                    bad |= (unsigned)__builtin_amdgcn_readfirstlane(table[min(key0 + b * 16, keys - 1) >> a.page_shift]) >= (unsigned)a.pages ? 1u << b : 0u;
+            }
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const int lim = (bad >> ((kb >> 1) * 2 + (lg >> 1))) & 1 ? -1 : last_key[qb];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key0 + (kb >> 1) * 32 + lg * 8 + (kb & 1) * 4 + i > lim) S[kb][qb][i] = -__builtin_inff();
+                }
+        }
+        float mx[QB];
+        bool over = false;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            mx[qb] = S[0][qb][0];
+#pragma unroll
+            for (int e = 1; e < 4 * KB; ++e) mx[qb] = __builtin_fmaxf(mx[qb], S[e / 4][qb][e % 4]);
+            over |= __builtin_fmaf(mx[qb], c, neg_mc[qb]) > MOVE_LOG2;
+        }
+        if (__builtin_amdgcn_ballot_w64(over) != 0) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                const float m_old = m_run[qb];
+                m_run[qb] = groups_max(__builtin_fmaxf(mx[qb], m_old));
+                neg_mc[qb] = -m_run[qb] * c;
+                const float alpha = __builtin_amdgcn_exp2f((m_old - m_run[qb]) * c);
+                L[qb] *= alpha;
+#pragma unroll
+                for (int fb = 0; fb < FB; ++fb) O[fb][qb] = O[fb][qb] * alpha;
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[kb][qb][2 * t], c, neg_mc[qb]));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(S[kb][qb][2 * t + 1], c, neg_mc[qb]));
+                    L[qb] += p0;
+                    L[qb] += p1;
+                    pw[kb / 2][qb][kb % 2 * 2 + t] = E::pack2(p0, p1);
+                }
+    };
+
+    // ---- the walk
+    constexpr std::true_type YES{};
+    constexpr std::false_type NO{};
+    if (nt > 0) {
+        issue_stage(-1);
+        issue_stage(0);
+        issue_stage(1);
+    }
+    // (Q is used once here, so that the compiler waits for its loads before the loop, and with them for the copies)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) asm volatile("" :: "v"(Qf[qb][kk]));
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    auto next = [&](int j) __attribute__((always_inline)) { if (j + 2 < nt) issue_stage(j + 2); };
+    if (nt_w == 0) {                            // no row of this wave sees a key of the split: it only copies
+        for (int j = 0; j < nt; ++j) {
+            wait_stage(j);
+            next(j);
+        }
+    } else if (!group_b) {
+        wait_stage(0);
+        burst(NO, YES, stage_ptr(-1));                                   // T_0
+        next(0);
+        int j = 0;                              // C_j is next
+        if (nt_full > 0 && !any_bad) {
+            softmax_tile(0, NO);
+            for (j = 1; j < nt_full && !any_bad; ++j) {
+                wait_stage(j);
+                burst(YES, YES, stage_ptr(j - 1));
+                next(j);
+                softmax_tile(j, NO);
+            }
+            if (j < nt_w) {
+                wait_stage(j);
+                burst(YES, YES, stage_ptr(j - 1));
+                next(j);
+            }
+        }
+        if (j < nt_w) {
+            softmax_tile(j, YES);
+            for (++j; j < nt_w; ++j) {
+                wait_stage(j);
+                careful_u(stage_ptr(j - 1));
+                burst(NO, YES, stage_ptr(j - 1));
+                next(j);
+                softmax_tile(j, YES);
+            }
+            if (j < nt) wait_stage(j);
+            careful_u(stage_ptr(j - 1));
+        } else {
+            if (j < nt) wait_stage(j);
+            burst(YES, NO, stage_ptr(j - 1));
+        }
+        if (j < nt) next(j);
+        for (++j; j < nt; ++j) {
+            wait_stage(j);
+            next(j);
+        }
+    } else {
+        burst(NO, YES, stage_ptr(-1));                                   // T_0
+        int j = 0;
+        for (; j < nt_full && j + 1 < nt_w && !any_bad; ++j) {
+            wait_stage(j);
+            next(j);
+            softmax_tile(j, NO);
+            burst(YES, YES, stage_ptr(j));
+        }
+        for (; j + 1 < nt_w; ++j) {
+            wait_stage(j);
+            next(j);
+            softmax_tile(j, YES);
+            careful_u(stage_ptr(j));
+            burst(NO, YES, stage_ptr(j));
+        }
+        wait_stage(j);                          // j == nt_w - 1
+        next(j);
+        softmax_tile(j, YES);
+        careful_u(stage_ptr(j));
+        for (++j; j < nt; ++j) {
+            wait_stage(j);
+            next(j);
+        }
+    }
+
+    // ---- results
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        L[qb] = groups_sum(L[qb]);
+        const int r = wq0 + qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group, t = seq.q0 + tok;
+        if (tok >= seq.n) continue;
+        const long long row = (long long)t * a.heads + head;
+        if (whole) {
+            const float inv = (L[qb] == 0.f ? 0.f : 1.f / L[qb]) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+            char* const to = a.o + t * a.o_token + head * a.o_head + lg * 8;
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb) {
+                const f32x4 x = O[fb][qb] * inv;
+                *reinterpret_cast<u32x2*>(to + fb * 32) = u32x2{E::pack2(x[0], x[1]), E::pack2(x[2], x[3])};
+            }
+            if (a.lse && lg == 0) a.lse[row] = m_run[qb] * scale + __builtin_logf(L[qb]);
+        } else {
+            const long long at = (long long)sp * a.tokens * a.heads + row;
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(a.part_o + at * D + fb * 16 + lg * 4) = O[fb][qb];
+            if (lg == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m_run[qb] * c, L[qb]};
+        }
+    }
+}
+
+template <int DTYPE, bool C8, int D>
+int launch(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
+{
+    constexpr int SMEM = STAGES * 2 * CachedRows<D, C8 ? 1 : 2, BN>::BYTES;
+    auto kern = attn_paged_chunk<DTYPE, C8, D>;
+    static PerDeviceOnce once;
+    if (once.prepare(reinterpret_cast<const void*>(kern), SMEM) < 0) return -1;
+    PagedArgs arg = a;
+    void* args[] = {&arg};
+    const long long grid = plan.chunk_tiles * a.chunk_splits * (a.heads / a.group);
+    return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, SMEM, stream) == hipSuccess ? 0 : -1;
+}
+
+}  // namespace
+
+int attn_paged_chunk_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream)
+{
+    const hipStream_t st = (hipStream_t)stream;
+    if (cache_dtype == KV_E4M3) {
+        if (dtype == 0) return d == 128 ? launch<0, true, 128>(a, plan, st) : launch<0, true, 64>(a, plan, st);
+        return d == 128 ? launch<1, true, 128>(a, plan, st) : launch<1, true, 64>(a, plan, st);
+    }
+    if (dtype == 0) return d == 128 ? launch<0, false, 128>(a, plan, st) : launch<0, false, 64>(a, plan, st);
+    return d == 128 ? launch<1, false, 128>(a, plan, st) : launch<1, false, 64>(a, plan, st);
+}

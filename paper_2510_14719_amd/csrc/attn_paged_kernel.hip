@@ -50,7 +50,7 @@ void attn_paged_few(PagedArgs a, int tiles)
     id /= a.splits;
     const int tile = id % tiles, s = id / tiles;
     const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-    if (tile * ROWS >= seq.n * a.group) return;
+    if (tile * ROWS >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
     const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal);
     const int k0 = sp * a.split, k1 = min(keys, k0 + a.split);
     if (sp > 0 && k0 >= keys) return;
@@ -308,7 +308,7 @@ void attn_paged_few(PagedArgs a, int tiles)
 // ---- the splits of a row joined: a wave a row
 template <int DTYPE, bool C8, int D>
 __global__ __launch_bounds__(256)
-void attn_paged_join(PagedArgs a, int rows)
+void attn_paged_join(PagedArgs a)
 {
     typedef Elem<DTYPE> E;
     constexpr int PL = D / 64;                  // features per lane
@@ -320,10 +320,12 @@ void attn_paged_join(PagedArgs a, int rows)
     if (s < 0) return;
     const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
     if (t < seq.q0 || t - seq.q0 >= seq.n) return;
+    const bool few = seq.n * a.group <= a.few_rows;
+    const int rows = few ? a.rows : PAGED_CHUNK_ROWS, split = few ? a.split : a.chunk_split;
     const int tile = ((t - seq.q0) * a.group + head % a.group) / rows;
     const int keys = paged_tile_keys(tile, rows, seq.n, a.group, seq.kv, a.causal);
-    if (keys <= a.split) return;
-    const int n = (keys + a.split - 1) / a.split;
+    if (keys <= split) return;
+    const int n = (keys + split - 1) / split;
     float m = -__builtin_inff(), l = 0.f, x[PL] = {};
     for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, a.part_ml[(i * all + row) * 2]);
     for (int i = 1; i < 64; i *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, i));
@@ -361,14 +363,16 @@ int launch_few(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 template <int DTYPE, bool C8, int D>
 int launch_all(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 {
-    int rc;
-    if (plan.rows == 16) rc = launch_few<DTYPE, C8, D, 1>(a, plan, stream);
-    else if (plan.rows == 32) rc = launch_few<DTYPE, C8, D, 2>(a, plan, stream);
-    else rc = launch_few<DTYPE, C8, D, 4>(a, plan, stream);
-    if (rc != 0 || a.splits == 1) return rc;
+    int rc = 0;
+    if (plan.tiles > 0) {
+        if (plan.rows == 16) rc = launch_few<DTYPE, C8, D, 1>(a, plan, stream);
+        else if (plan.rows == 32) rc = launch_few<DTYPE, C8, D, 2>(a, plan, stream);
+        else rc = launch_few<DTYPE, C8, D, 4>(a, plan, stream);
+    }
+    if (rc == 0 && plan.chunk_tiles > 0) rc = attn_paged_chunk_launch(a, plan, D, DTYPE, C8 ? KV_E4M3 : DTYPE, stream);
+    if (rc != 0 || (a.splits == 1 && a.chunk_splits == 1)) return rc;
     PagedArgs arg = a;
-    int rows = plan.rows;
-    void* args[] = {&arg, &rows};
+    void* args[] = {&arg};
     const unsigned grid = (unsigned)(((long long)a.tokens * a.heads + 3) / 4);
     return hipLaunchKernel(reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D>), dim3(grid), dim3(256), args, 0, stream) == hipSuccess ? 0 : -1;
 }
@@ -377,18 +381,36 @@ int launch_all(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes)
 {
-    (void)tokens; (void)d; (void)cache_bytes;
-    const long long most = (long long)max_q * (heads / key_heads);
-    PagedPlan p;
+    (void)d; (void)cache_bytes;
+    const int group = heads / key_heads;
+    const long long most = (long long)max_q * group;
+    const int whole = (max_kv + 127) / 128 * 128;            // one split
+    PagedPlan p{};
     p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-    p.tiles = (int)((most + p.rows - 1) / p.rows);
-    // Keys per split: so many that about 8 workgroups a compute unit come out if all sequences are long, 512 at least.
-    const long long units = (long long)sequences * p.tiles * key_heads;
-    long long split = (units * max_kv / (8 * 256) + 127) / 128 * 128;
-    if (split < 512) split = 512;
-    if (split > max_kv) split = (max_kv + 127) / 128 * 128;
-    p.split = (int)split;
-    p.splits = (int)((max_kv + split - 1) / split);
+    p.splits = p.chunk_splits = 1;
+    p.split = p.chunk_split = whole;
+    // Sequences of up to 64 rows take small tiles, longer ones chunks.  One sequence takes one kind.
+    p.few_rows = most <= 64 || sequences > 1 ? 64 : 0;
+    p.tiles = p.few_rows ? 1 : 0;
+    if (p.tiles) {
+        // Keys per split: so many that about 8 workgroups a compute unit come out if all sequences are long, 512 at least.
+        const long long units = (long long)sequences * key_heads;
+        long long split = (units * max_kv / (8 * 256) + 127) / 128 * 128;
+        if (split < 512) split = 512;
+        p.split = (int)(split > whole ? whole : split);
+        p.splits = (int)((max_kv + p.split - 1) / p.split);
+    }
+    if (most > 64) {
+        const long long each = (most + PAGED_CHUNK_ROWS - 1) / PAGED_CHUNK_ROWS * sequences, all = (long long)tokens * group / PAGED_CHUNK_ROWS + sequences;
+        p.chunk_tiles = each < all ? each : all;
+        const long long units = p.chunk_tiles * key_heads;
+        if (units < 256) {
+            long long split = (units * max_kv / 512 + 127) / 128 * 128;
+            if (split < 512) split = 512;
+            p.chunk_split = (int)(split > whole ? whole : split);
+            p.chunk_splits = (int)((max_kv + p.chunk_split - 1) / p.chunk_split);
+        }
+    }
     return p;
 }
 

@@ -133,13 +133,14 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 // Floats per row and split of partial results: O, reference and sum.
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
-    return p.splits > 1 ? (i64)p.splits * b->tokens * heads * (c->d + 2) * 4 : 0;
+    const int splits = p.splits > p.chunk_splits ? p.splits : p.chunk_splits;
+    return splits > 1 ? (i64)splits * b->tokens * heads * (c->d + 2) * 4 : 0;
 }
 bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
     const i64 most = 1ll << 23;                 // workgroups of 512 threads: a grid has less than 2^32
-    if ((i64)p.tiles * p.splits >= most || (i64)p.tiles * p.splits * c->heads >= most) return false;
-    return (i64)p.tiles * p.splits * c->heads * b->sequences < most && ((i64)b->tokens * heads + 3) / 4 < 2 * most;
+    auto fits = [&](i64 tiles, i64 splits) { return tiles < most && tiles * splits < most && tiles * splits * c->heads < most; };
+    return fits(p.tiles, b->sequences) && fits((i64)p.tiles * b->sequences, p.splits) && fits(p.chunk_tiles, p.chunk_splits) && ((i64)b->tokens * heads + 3) / 4 < 2 * most;
 }
 
 int check_book(const kv_book* b)
@@ -235,7 +236,7 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.o_token = o->token_stride * 2;
     a.o_head = o->head_stride * 2;
     a.part_o = (float*)workspace;
-    a.part_ml = (float*)workspace + (i64)p.splits * batch->tokens * heads * cache->d;
+    a.part_ml = (float*)workspace + (i64)(p.splits > p.chunk_splits ? p.splits : p.chunk_splits) * batch->tokens * heads * cache->d;
     a.sequences = batch->sequences;
     a.tokens = batch->tokens;
     a.table_stride = batch->table_stride;
@@ -246,8 +247,12 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.heads = heads;
     a.group = heads / cache->heads;
     a.causal = causal != 0;
+    a.few_rows = p.few_rows;
+    a.rows = p.rows;
     a.split = p.split;
     a.splits = p.splits;
+    a.chunk_split = p.chunk_split;
+    a.chunk_splits = p.chunk_splits;
     a.scale = scale;
     return launched(attn_paged_launch(a, p, cache->d, dtype, cache->dtype, stream));
 }

@@ -22,15 +22,20 @@ struct PagedArgs {
     float *part_o, *part_ml;                                 // partial results: [split][token * heads + head][d], [..][2]
     int sequences, tokens, table_stride, max_q, max_kv, pages, page_shift;
     int heads, group;                                        // query heads, and how many share a key head
-    int causal, split, splits;                               // keys per split (a multiple of 128), splits of the longest sequence
+    int causal;
+    int few_rows;                                            // sequences with more rows (new tokens x group) than this go by chunks of PAGED_CHUNK_ROWS
+    int rows, split, splits;                                 // the others: rows per workgroup, keys per split (a multiple of 128), splits of the longest sequence
+    int chunk_split, chunk_splits;
     float scale;
 };
 
+constexpr int PAGED_CHUNK_ROWS = 256;                        // query rows (tokens x heads of a group) of a workgroup of attn_paged_chunk
+
 // How a call is laid out (chosen by its sizes alone, so that the workspace is known beforehand).
 struct PagedPlan {
-    int rows;                                                // query rows (tokens x heads of a group) per workgroup
-    int tiles;                                               // row tiles of the sequence with the most new tokens
-    int split, splits;
+    int few_rows, rows, split, splits, chunk_split, chunk_splits;        // as in PagedArgs
+    int tiles;                                               // workgroups of `rows` rows for a sequence; 0: all go by chunks
+    long long chunk_tiles;                                   // chunks of all sequences, at most; 0: none does
 };
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes);
 
@@ -45,6 +50,7 @@ PAGED_HD inline int paged_tile_keys(int tile, int rows, int n, int group, int kv
 }
 
 // Enqueue for validated arguments: 0, or -1 if HIP refused a launch.
+int attn_paged_chunk_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream);
 int attn_paged_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream);
 
 struct RopeArgs {

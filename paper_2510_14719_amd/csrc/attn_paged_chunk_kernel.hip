@@ -40,42 +40,29 @@ void attn_paged_chunk(PagedArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lc = lane & 15, lg = lane >> 4;
     const bool group_b = wave >= NW / 2;
 
-    // ---- which rows: tiles of the sequences that are long enough, numbered through; long ones (late tokens) first inside a sequence
-    const int key_heads = a.heads / a.group;
-    int id = blockIdx.x;
-    const int h = id % key_heads;
-    id /= key_heads;
-    const int sp = id % a.chunk_splits;
-    int left = id / a.chunk_splits, s = -1, tile = 0;
-    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
-        int mine = 0;
-        if (s0 + lane < a.sequences) {
-            const int rows = seq_range(a.q_start, a.kv_len, s0 + lane, a.tokens, a.max_q, a.max_kv).n * a.group;
-            mine = rows > a.few_rows ? (rows + BM - 1) / BM : 0;
-        }
-        int sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int x = __shfl_up(sum, d);
-            if (lane >= d) sum += x;
-        }
-        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(sum > left);
-        if (beyond) {
-            const int at = __builtin_ctzll(beyond);
-            s = s0 + at;
-            tile = __builtin_amdgcn_readlane(sum, at) - 1 - left;        // (from the last to the first)
-            break;
-        }
-        left -= __builtin_amdgcn_readlane(sum, 63);
+    // ---- which chunk, and which piece of its keys
+    const int key_heads = a.heads / a.group, h = blockIdx.x % key_heads;
+    const ChunkSeq first = chunk_seq(a, lane);
+    const ChunkCut cut = chunk_cut(a, first, key_heads, lane);
+    const ChunkPiece mine = chunk_numbered(a, first, cut.inverse, blockIdx.x / key_heads, lane);
+    const int s = __builtin_amdgcn_readfirstlane(mine.s), tile = __builtin_amdgcn_readfirstlane(mine.chunk);
+    int keys = 0, per = 0;                      // keys of the chunk, of a piece
+    SeqRange seq = {0, 0, 0};
+    if (s >= 0) {
+        seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+        keys = __builtin_amdgcn_readfirstlane(paged_tile_keys(tile, BM, seq.n, a.group, seq.kv, a.causal));
+        per = chunk_piece_tiles(mine.pieces, keys) * BN;
+    }
+    if (threadIdx.x == 0 && a.chunk_parts > 0) {                         // for attn_paged_join_chunks
+        if (blockIdx.x == 0) a.chunk_what[a.chunk_parts * 4] = cut.chunks * key_heads;
+        if (cut.chunks > 0 && s >= 0 && mine.piece == 0)
+            *reinterpret_cast<u32x4*>(a.chunk_what + (mine.number * key_heads + h) * 4) =
+                u32x4{(unsigned)s, (unsigned)tile, (unsigned)(per < keys ? (keys + per - 1) / per : 1), blockIdx.x};
     }
     if (s < 0) return;
-    s = __builtin_amdgcn_readfirstlane(s);
-    tile = __builtin_amdgcn_readfirstlane(tile);
-    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-    const int keys = __builtin_amdgcn_readfirstlane(paged_tile_keys(tile, BM, seq.n, a.group, seq.kv, a.causal));
-    const int k0 = sp * a.chunk_split, k1 = min(keys, k0 + a.chunk_split);
-    if (sp > 0 && k0 >= keys) return;
-    const bool whole = keys <= a.chunk_split;
+    const int k0 = __builtin_amdgcn_readfirstlane(mine.piece * per), k1 = __builtin_amdgcn_readfirstlane(min(keys, k0 + per));
+    if (mine.piece > 0 && k0 >= keys) return;
+    const bool whole = per >= keys;
 
     // ---- rows of this wave, lane % 16 of each 16-row block
     const int wq0 = tile * BM + wave * (QB * 16);
@@ -322,6 +309,8 @@ void attn_paged_chunk(PagedArgs a)
     wait_vmcnt<0>();
     __builtin_amdgcn_s_barrier();
     auto next = [&](int j) __attribute__((always_inline)) { if (j + 2 < nt) issue_stage(j + 2); };
+    // (the last tile of a wave is none of these: it is always done with care)
+    auto whole_tiles = [&](int j) __attribute__((always_inline)) { return j < nt_full && j + 1 < nt_w && !any_bad; };
     if (nt_w == 0) {                            // no row of this wave sees a key of the split: it only copies
         for (int j = 0; j < nt; ++j) {
             wait_stage(j);
@@ -332,36 +321,21 @@ void attn_paged_chunk(PagedArgs a)
         burst(NO, YES, stage_ptr(-1));                                   // T_0
         next(0);
         int j = 0;                              // C_j is next
-        if (nt_full > 0 && !any_bad) {
-            softmax_tile(0, NO);
-            for (j = 1; j < nt_full && !any_bad; ++j) {
-                wait_stage(j);
-                burst(YES, YES, stage_ptr(j - 1));
-                next(j);
+        if (whole_tiles(0)) {
+            do {                                // (bottom-tested, here and below: the accumulators stay in place)
                 softmax_tile(j, NO);
-            }
-            if (j < nt_w) {
-                wait_stage(j);
+                wait_stage(++j);
                 burst(YES, YES, stage_ptr(j - 1));
                 next(j);
-            }
+            } while (whole_tiles(j));
         }
-        if (j < nt_w) {
+        do {
             softmax_tile(j, YES);
-            for (++j; j < nt_w; ++j) {
-                wait_stage(j);
-                careful_u(stage_ptr(j - 1));
-                burst(NO, YES, stage_ptr(j - 1));
-                next(j);
-                softmax_tile(j, YES);
-            }
-            if (j < nt) wait_stage(j);
+            if (++j < nt) wait_stage(j);
             careful_u(stage_ptr(j - 1));
-        } else {
-            if (j < nt) wait_stage(j);
-            burst(YES, NO, stage_ptr(j - 1));
-        }
-        if (j < nt) next(j);
+            if (j < nt_w) burst(NO, YES, stage_ptr(j - 1));
+            next(j);
+        } while (j < nt_w);
         for (++j; j < nt; ++j) {
             wait_stage(j);
             next(j);
@@ -369,24 +343,22 @@ void attn_paged_chunk(PagedArgs a)
     } else {
         burst(NO, YES, stage_ptr(-1));                                   // T_0
         int j = 0;
-        for (; j < nt_full && j + 1 < nt_w && !any_bad; ++j) {
-            wait_stage(j);
-            next(j);
-            softmax_tile(j, NO);
-            burst(YES, YES, stage_ptr(j));
+        if (whole_tiles(0)) {
+            do {
+                wait_stage(j);
+                next(j);
+                softmax_tile(j, NO);
+                burst(YES, YES, stage_ptr(j));
+            } while (whole_tiles(++j));
         }
-        for (; j + 1 < nt_w; ++j) {
+        do {
             wait_stage(j);
             next(j);
             softmax_tile(j, YES);
             careful_u(stage_ptr(j));
-            burst(NO, YES, stage_ptr(j));
-        }
-        wait_stage(j);                          // j == nt_w - 1
-        next(j);
-        softmax_tile(j, YES);
-        careful_u(stage_ptr(j));
-        for (++j; j < nt; ++j) {
+            if (j + 1 < nt_w) burst(NO, YES, stage_ptr(j));
+        } while (++j < nt_w);
+        for (; j < nt; ++j) {
             wait_stage(j);
             next(j);
         }
@@ -409,10 +381,10 @@ void attn_paged_chunk(PagedArgs a)
             }
             if (a.lse && lg == 0) a.lse[row] = m_run[qb] * scale + __builtin_logf(L[qb]);
         } else {
-            const long long at = (long long)sp * a.tokens * a.heads + row;
+            const long long at = (long long)blockIdx.x * BM + r % BM;
 #pragma unroll
-            for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(a.part_o + at * D + fb * 16 + lg * 4) = O[fb][qb];
-            if (lg == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m_run[qb] * c, L[qb]};
+            for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(a.chunk_o + at * D + fb * 16 + lg * 4) = O[fb][qb];
+            if (lg == 0) *reinterpret_cast<f32x2*>(a.chunk_ml + at * 2) = f32x2{m_run[qb] * c, L[qb]};
         }
     }
 }
@@ -426,7 +398,7 @@ int launch(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
     if (once.prepare(reinterpret_cast<const void*>(kern), SMEM) < 0) return -1;
     PagedArgs arg = a;
     void* args[] = {&arg};
-    const long long grid = plan.chunk_tiles * a.chunk_splits * (a.heads / a.group);
+    const long long grid = plan.chunk_tiles > a.chunk_parts ? plan.chunk_tiles : a.chunk_parts;
     return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, SMEM, stream) == hipSuccess ? 0 : -1;
 }
 

@@ -19,9 +19,8 @@ namespace {
 
 // The softmax reference moves only when a row maximum grew by more than this many powers of two.
 constexpr float MOVE_LOG2 = 8.0f;
-constexpr int NW = 4;                           // waves of a workgroup
 
-template <int D, int ES, int QB> struct FewLayout {
+template <int D, int ES, int QB, int NW> struct FewLayout {
     typedef CachedRows<D, ES, 32> Rows;
     static constexpr int STAGE = 2 * Rows::BYTES, SLOTS = 2, RING = NW * SLOTS * STAGE;
     static constexpr int JOIN = NW * (D / 16) * QB * 1024;   // O of every wave
@@ -29,12 +28,12 @@ template <int D, int ES, int QB> struct FewLayout {
     static constexpr int SMEM = (RING > JOIN ? RING : JOIN) + SUMS;
 };
 
-template <int DTYPE, bool C8, int D, int QB>
+template <int DTYPE, bool C8, int D, int QB, int NW>
 __global__ __launch_bounds__(NW * 64)
-void attn_paged_few(PagedArgs a, int tiles)
+void attn_paged_few(PagedArgs a)
 {
     typedef Elem<DTYPE> E;
-    typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
+    typedef FewLayout<D, C8 ? 1 : 2, QB, NW> Layout;
     typedef typename Layout::Rows Rows;
     constexpr int KK = D / 32, FB = D / 16, ROWS = QB * 16;
     constexpr int SUBS = 16 / Rows::PER_PIECE;               // pieces of 16 keys and a line of their rows
@@ -46,13 +45,19 @@ void attn_paged_few(PagedArgs a, int tiles)
     int id = blockIdx.x;
     const int h = id % key_heads;
     id /= key_heads;
-    const int sp = id % a.splits;
-    id /= a.splits;
-    const int tile = id % tiles, s = id / tiles;
+    const int sp = id % a.splits, s = id / a.splits;
+    // ---- the wave's steps are 32 keys each, every NW-th of the split's.  Their table entries are asked for before the sequence's length is known.
+    const int k0 = sp * a.split;
+    const int* const table = a.table + (long long)s * a.table_stride;
+    auto entries_of = [&](int step) __attribute__((always_inline)) {     // lane 2 i + hf: page of half hf of the i-th step from here
+        const int key = min(k0 + ((step + (lane >> 1)) * NW + wave) * 32 + (lane & 1) * 16, a.max_kv - 1);
+        return table[key >> a.page_shift];
+    };
+    int entries = entries_of(0);
     const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-    if (tile * ROWS >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal);
-    const int k0 = sp * a.split, k1 = min(keys, k0 + a.split);
+    if (seq.n == 0 || seq.n * a.group > a.few_rows) return;
+    const int keys = paged_tile_keys(0, ROWS, seq.n, a.group, seq.kv, a.causal);
+    const int k1 = min(keys, k0 + a.split);
     if (sp > 0 && k0 >= keys) return;
     const bool whole = keys <= a.split;
 
@@ -62,7 +67,7 @@ void attn_paged_few(PagedArgs a, int tiles)
     long long o_row[QB];                        // token * heads + head, -1 behind the last row
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int r = tile * ROWS + qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group;
+        const int r = qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group;
         const bool real = tok < seq.n;
         const int t = seq.q0 + (real ? tok : seq.n - 1);
         const char* const at = a.q + t * a.q_token + head * a.q_head + lg * 16;
@@ -71,7 +76,7 @@ void attn_paged_few(PagedArgs a, int tiles)
         last_key[qb] = a.causal ? min(seq.kv - seq.n + tok, keys - 1) : keys - 1;
         o_row[qb] = real ? (long long)t * a.heads + head : -1;
     }
-    const int first_last = a.causal ? seq.kv - seq.n + tile * ROWS / a.group : keys - 1;   // what the first row sees
+    const int first_last = a.causal ? seq.kv - seq.n : keys - 1;   // what the first row sees
 
     const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
     // The reference before the first score: the most negative float whose scaled value is finite.  (-inf would make NaN of rows whose
@@ -88,15 +93,8 @@ void attn_paged_few(PagedArgs a, int tiles)
         for (int fb = 0; fb < FB; ++fb) O[fb][qb] = f32x4(0.f);
     }
 
-    // ---- the wave's steps: 32 keys each, every NW-th of the split's
     const int blocks = (k1 - k0 + 31) / 32, steps = blocks > wave ? (blocks - wave + NW - 1) / NW : 0;
-    const int* const table = a.table + (long long)s * a.table_stride;
     const int page_mask = (1 << a.page_shift) - 1;
-    int entries = 0;                            // lane 2 i + hf: page of half hf of the i-th step of the current 32
-    auto load_entries = [&](int step) __attribute__((always_inline)) {
-        const int key = min(k0 + ((step + (lane >> 1)) * NW + wave) * 32 + (lane & 1) * 16, keys - 1);
-        entries = table[key >> a.page_shift];
-    };
     // per-lane source offsets of a copy inside 16 keys: row and (permuted) column
     unsigned k_off[2][SUBS], v_off[2][SUBS];
 #pragma unroll
@@ -116,12 +114,13 @@ void attn_paged_few(PagedArgs a, int tiles)
         unsigned bad = 0;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            int page = __builtin_amdgcn_readlane(entries, (step & 31) * 2 + hf);
+            const int k_half = key + hf * 16;
+            // (a half behind the last key takes the other one's page: the last key's)
+            int page = __builtin_amdgcn_readlane(entries, (step & 31) * 2 + (k_half < keys ? hf : 0));
             if ((unsigned)page >= (unsigned)a.pages) {
                 page = 0;
                 bad |= 1u << hf;
             }
-            const int k_half = key + hf * 16;
             long long off = page * a.page_bytes;
             if (k_half + 16 <= keys) {
                 off += (k_half & page_mask) * a.token_bytes;
@@ -151,8 +150,7 @@ void attn_paged_few(PagedArgs a, int tiles)
         return bad;
     };
 
-    if (steps > 0) load_entries(0);
-    // Q is used once here, so that the compiler waits for its loads (and the entries') before the first copy and not for all copies later.
+    // Q is used once here, so that the compiler waits for its loads before the first copy and not for all copies later.
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
@@ -249,13 +247,13 @@ void attn_paged_few(PagedArgs a, int tiles)
         }
         bad = bad_next;
         if (step + 2 < steps) {
-            if (((step + 2) & 31) == 0) load_entries(step + 2);
+            if (((step + 2) & 31) == 0) entries = entries_of(step + 2);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // every read of the slot is done
             bad_next = issue(step + 2);
         }
     }
 
-    // ---- join the waves: each takes a quarter of the features
+    // ---- join the waves: each takes its share of the features
     float* const sums = reinterpret_cast<float*>(smem + Layout::SMEM - Layout::SUMS);
     __syncthreads();
 #pragma unroll
@@ -305,58 +303,100 @@ void attn_paged_few(PagedArgs a, int tiles)
     }
 }
 
-// ---- the splits of a row joined: a wave a row
-template <int DTYPE, bool C8, int D>
-__global__ __launch_bounds__(256)
+// ---- the splits of a row joined: WAVES waves (a workgroup) a row.  Groups of D / 4 lanes take 16 bytes each of a part's O, so that several parts are under
+// way at a time, and the groups' sums meet in the LDS.
+template <int DTYPE, bool C8, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * 64)
 void attn_paged_join(PagedArgs a)
 {
     typedef Elem<DTYPE> E;
-    constexpr int PL = D / 64;                  // features per lane
-    const int lane = threadIdx.x & 63;
-    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), all = (long long)a.tokens * a.heads;
-    if (row >= all) return;
-    const int t = (int)(row / a.heads), head = (int)(row % a.heads);
-    const int s = seq_of_token(a.q_start, a.sequences, t, lane);
-    if (s < 0) return;
-    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-    if (t < seq.q0 || t - seq.q0 >= seq.n) return;
-    const bool few = seq.n * a.group <= a.few_rows;
-    const int rows = few ? a.rows : PAGED_CHUNK_ROWS, split = few ? a.split : a.chunk_split;
-    const int tile = ((t - seq.q0) * a.group + head % a.group) / rows;
-    const int keys = paged_tile_keys(tile, rows, seq.n, a.group, seq.kv, a.causal);
-    if (keys <= split) return;
-    const int n = (keys + split - 1) / split;
-    float m = -__builtin_inff(), l = 0.f, x[PL] = {};
-    for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, a.part_ml[(i * all + row) * 2]);
+    constexpr int LANES = D / 4, GROUPS = WAVES * 64 / LANES;
+    __shared__ f32x4 s_x[GROUPS][LANES];
+    __shared__ float s_l[GROUPS];
+    const int lane = threadIdx.x & 63, group = threadIdx.x / LANES, e = threadIdx.x % LANES;
+    // the r-th row of key head h of sequence s
+    const int key_heads = a.heads / a.group, most = min(a.rows, a.max_q * a.group), r = blockIdx.x % most, h = blockIdx.x / most % key_heads;
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, blockIdx.x / most / key_heads, a.tokens, a.max_q, a.max_kv);
+    if (r >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
+    const int keys = paged_tile_keys(0, a.rows, seq.n, a.group, seq.kv, a.causal);
+    if (keys <= a.split) return;
+    const int n = (keys + a.split - 1) / a.split, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
+    const long long row = (long long)t * a.heads + head, all = (long long)a.tokens * a.heads;
+    const float* const part_o = a.part_o + row * D;
+    const float* const part_ml = a.part_ml + row * 2;
+    float m = -__builtin_inff();
+    for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, part_ml[i * all * 2]);
+#pragma unroll
     for (int i = 1; i < 64; i *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, i));
     // (every part has a finite reference, so m is finite)
+    f32x4 x = f32x4(0.f);
+    float l = 0.f;
 #pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + (i * all + row) * 2);
+    for (int i = group; i < n; i += GROUPS) {
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(part_ml + i * all * 2);
         const float w = __builtin_amdgcn_exp2f(ml[0] - m);
         l += ml[1] * w;
-#pragma unroll
-        for (int e = 0; e < PL; ++e) x[e] += a.part_o[(i * all + row) * D + lane * PL + e] * w;
+        x += *reinterpret_cast<const f32x4*>(part_o + i * all * D + e * 4) * w;
     }
-    const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[head / a.group] : 1.f);
-    char* const dst = a.o + t * a.o_token + head * a.o_head;
-    const unsigned y = E::pack2(x[0] * inv, x[PL - 1] * inv);
-    if constexpr (PL == 2) reinterpret_cast<unsigned*>(dst)[lane] = y;
-    else reinterpret_cast<uint16_t*>(dst)[lane] = (uint16_t)y;
-    if (a.lse && lane == 0) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    s_x[group][e] = x;
+    if (e == 0) s_l[group] = l;
+    __syncthreads();
+    if (threadIdx.x >= LANES) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+        x += s_x[g][e];
+        l += s_l[g];
+    }
+    const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+    *reinterpret_cast<u32x2*>(a.o + t * a.o_token + head * a.o_head + e * 8) = u32x2{E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};
+    if (a.lse && e == 0) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <int DTYPE, bool C8, int D, int QB>
-int launch_few(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
+// ---- the pieces of a chunk joined: D / 4 lanes a row, so 1024 / D rows by a workgroup
+template <int DTYPE, bool C8, int D>
+__global__ __launch_bounds__(256)
+void attn_paged_join_chunks(PagedArgs a)
 {
-    typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
-    auto kern = attn_paged_few<DTYPE, C8, D, QB>;
+    typedef Elem<DTYPE> E;
+    constexpr int LANES = D / 4;
+    const int key_heads = a.heads / a.group, h = blockIdx.x % key_heads, e = threadIdx.x % LANES;
+    if ((int)blockIdx.x >= a.chunk_what[a.chunk_parts * 4]) return;
+    const u32x4 what = *reinterpret_cast<const u32x4*>(a.chunk_what + blockIdx.x * 4);
+    const int s = (int)what[0], n = (int)what[2];            // (a chunk is cut into 14 pieces at most)
+    if (n < 2) return;
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    const long long step = (long long)key_heads * PAGED_CHUNK_ROWS;      // from a piece to the next
+    const int r = blockIdx.y * (256 / LANES) + threadIdx.x / LANES, row = (int)what[1] * PAGED_CHUNK_ROWS + r, tok = row / a.group, head = h * a.group + row % a.group;
+    if (tok >= seq.n) return;
+    const long long first = (long long)what[3] * PAGED_CHUNK_ROWS + r;
+    const int k = min(threadIdx.x & 15, n - 1);
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.chunk_ml + (first + k * step) * 2);       // a piece a lane
+    float m = ml[0];
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+    const float w = __builtin_amdgcn_exp2f(ml[0] - m);
+    float l = (int)(threadIdx.x & 15) < n ? ml[1] * w : 0.f;
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
+    f32x4 x = f32x4(0.f);
+#pragma unroll 7
+    for (int j = 0; j < n; ++j) x += *reinterpret_cast<const f32x4*>(a.chunk_o + (first + j * step) * D + e * 4) * __shfl(w, (threadIdx.x & 48) + j);
+    const int t = seq.q0 + tok;
+    const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+    *reinterpret_cast<u32x2*>(a.o + t * a.o_token + head * a.o_head + e * 8) = u32x2{E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};
+    if (a.lse && e == 0) a.lse[(long long)t * a.heads + head] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int DTYPE, bool C8, int D, int QB, int NW>
+int launch_few(const PagedArgs& a, hipStream_t stream)
+{
+    typedef FewLayout<D, C8 ? 1 : 2, QB, NW> Layout;
+    auto kern = attn_paged_few<DTYPE, C8, D, QB, NW>;
     static PerDeviceOnce once;
     if (once.prepare(reinterpret_cast<const void*>(kern), Layout::SMEM) < 0) return -1;
     PagedArgs arg = a;
-    int tiles = plan.tiles;
-    void* args[] = {&arg, &tiles};
-    const long long grid = (long long)a.sequences * tiles * a.splits * (a.heads / a.group);
+    void* args[] = {&arg};
+    const long long grid = (long long)a.sequences * a.splits * (a.heads / a.group);
     return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, Layout::SMEM, stream) == hipSuccess ? 0 : -1;
 }
 
@@ -364,52 +404,47 @@ template <int DTYPE, bool C8, int D>
 int launch_all(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 {
     int rc = 0;
-    if (plan.tiles > 0) {
-        if (plan.rows == 16) rc = launch_few<DTYPE, C8, D, 1>(a, plan, stream);
-        else if (plan.rows == 32) rc = launch_few<DTYPE, C8, D, 2>(a, plan, stream);
-        else rc = launch_few<DTYPE, C8, D, 4>(a, plan, stream);
-    }
+    if (plan.waves == 4) rc = plan.rows == 16 ? launch_few<DTYPE, C8, D, 1, 4>(a, stream) : launch_few<DTYPE, C8, D, 2, 4>(a, stream);
+    if (plan.waves == 2) rc = plan.rows == 16 ? launch_few<DTYPE, C8, D, 1, 2>(a, stream) : launch_few<DTYPE, C8, D, 2, 2>(a, stream);
     if (rc == 0 && plan.chunk_tiles > 0) rc = attn_paged_chunk_launch(a, plan, D, DTYPE, C8 ? KV_E4M3 : DTYPE, stream);
-    if (rc != 0 || (a.splits == 1 && a.chunk_splits == 1)) return rc;
     PagedArgs arg = a;
     void* args[] = {&arg};
-    const unsigned grid = (unsigned)(((long long)a.tokens * a.heads + 3) / 4);
-    return hipLaunchKernel(reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D>), dim3(grid), dim3(256), args, 0, stream) == hipSuccess ? 0 : -1;
+    if (rc == 0 && a.chunk_parts > 0)
+        rc = hipLaunchKernel(reinterpret_cast<const void*>(attn_paged_join_chunks<DTYPE, C8, D>), dim3((unsigned)(plan.chunk_tiles < a.chunk_parts ? plan.chunk_tiles : a.chunk_parts), PAGED_CHUNK_ROWS / (1024 / D)), dim3(256), args, 0, stream) == hipSuccess ? 0 : -1;
+    if (rc != 0 || a.splits == 1) return rc;
+    // (few rows: 4 waves a row, to have many parts under way; many: one)
+    const int most = a.max_q * a.group < a.rows ? a.max_q * a.group : a.rows;
+    const long long grid = (long long)a.sequences * (a.heads / a.group) * most;
+    const void* const kern = grid <= 1024 ? reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D, 4>) : reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D, 1>);
+    return hipLaunchKernel(kern, dim3((unsigned)grid), dim3(grid <= 1024 ? 256 : 64), args, 0, stream) == hipSuccess ? 0 : -1;
 }
 
 }  // namespace
 
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes)
 {
-    (void)d; (void)cache_bytes;
     const int group = heads / key_heads;
     const long long most = (long long)max_q * group;
     const int whole = (max_kv + 127) / 128 * 128;            // one split
     PagedPlan p{};
-    p.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
-    p.splits = p.chunk_splits = 1;
-    p.split = p.chunk_split = whole;
-    // Sequences of up to 64 rows take small tiles, longer ones chunks.  One sequence takes one kind.
-    p.few_rows = most <= 64 || sequences > 1 ? 64 : 0;
-    p.tiles = p.few_rows ? 1 : 0;
-    if (p.tiles) {
-        // Keys per split: so many that about 8 workgroups a compute unit come out if all sequences are long, 512 at least.
-        const long long units = (long long)sequences * key_heads;
-        long long split = (units * max_kv / (8 * 256) + 127) / 128 * 128;
+    p.splits = 1;
+    p.split = whole;
+    // Sequences of up to 32 rows take small tiles, longer ones chunks.  One sequence takes one kind.
+    p.rows = most <= 16 ? 16 : 32;
+    p.few_rows = most <= 32 || (long long)sequences * key_heads > 64 ? 32 : 0;
+    if (p.few_rows) {
+        const long long units = (long long)sequences * key_heads, most_keys = (768 << 10) / (2 * d * cache_bytes);
+        long long split = units >= 512 ? most_keys : (units * max_kv / 1024 + 127) / 128 * 128;
+        if (split > most_keys) split = most_keys;
         if (split < 512) split = 512;
-        p.split = (int)(split > whole ? whole : split);
+        if (max_kv > 1024 && split < whole) p.split = (int)split;
         p.splits = (int)((max_kv + p.split - 1) / p.split);
+        p.waves = units * p.splits <= 256 ? 4 : 2;
     }
-    if (most > 64) {
+    if (most > 32) {
         const long long each = (most + PAGED_CHUNK_ROWS - 1) / PAGED_CHUNK_ROWS * sequences, all = (long long)tokens * group / PAGED_CHUNK_ROWS + sequences;
-        p.chunk_tiles = each < all ? each : all;
-        const long long units = p.chunk_tiles * key_heads;
-        if (units < 256) {
-            long long split = (units * max_kv / 512 + 127) / 128 * 128;
-            if (split < 512) split = 512;
-            p.chunk_split = (int)(split > whole ? whole : split);
-            p.chunk_splits = (int)((max_kv + p.chunk_split - 1) / p.chunk_split);
-        }
+        p.chunk_tiles = (each < all ? each : all) * key_heads;
+        if (max_kv > CHUNK_UNCUT) p.chunk_parts = CHUNK_PARTS;
     }
     return p;
 }

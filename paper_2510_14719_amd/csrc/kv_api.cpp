@@ -130,17 +130,17 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 {
     return paged_plan(b->sequences, b->tokens, max_q_of(b), b->max_kv, heads, c->heads, c->d, c->dtype == KV_E4M3 ? 1 : 2);
 }
-// Floats per row and split of partial results: O, reference and sum.
+// Rows of partial results, d + 2 floats each (O, reference and sum): of the small tiles, and of the chunks.
+i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? (i64)p.splits * b->tokens * heads : 0; }
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
-    const int splits = p.splits > p.chunk_splits ? p.splits : p.chunk_splits;
-    return splits > 1 ? (i64)splits * b->tokens * heads * (c->d + 2) * 4 : 0;
+    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0);
 }
 bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
     const i64 most = 1ll << 23;                 // workgroups of 512 threads: a grid has less than 2^32
     auto fits = [&](i64 tiles, i64 splits) { return tiles < most && tiles * splits < most && tiles * splits * c->heads < most; };
-    return fits(p.tiles, b->sequences) && fits((i64)p.tiles * b->sequences, p.splits) && fits(p.chunk_tiles, p.chunk_splits) && ((i64)b->tokens * heads + 3) / 4 < 2 * most;
+    return fits(p.splits, b->sequences) && fits(p.chunk_tiles, 1) && fits(b->sequences, p.rows);
 }
 
 int check_book(const kv_book* b)
@@ -235,8 +235,12 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.q_head = q->head_stride * 2;
     a.o_token = o->token_stride * 2;
     a.o_head = o->head_stride * 2;
+    const i64 few = few_parts(p, batch, heads), chunk = (i64)p.chunk_parts * PAGED_CHUNK_ROWS;
     a.part_o = (float*)workspace;
-    a.part_ml = (float*)workspace + (i64)(p.splits > p.chunk_splits ? p.splits : p.chunk_splits) * batch->tokens * heads * cache->d;
+    a.chunk_o = a.part_o + few * cache->d;
+    a.part_ml = a.chunk_o + chunk * cache->d;
+    a.chunk_ml = a.part_ml + few * 2;
+    a.chunk_what = (int*)(a.chunk_ml + chunk * 2);
     a.sequences = batch->sequences;
     a.tokens = batch->tokens;
     a.table_stride = batch->table_stride;
@@ -251,8 +255,7 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.rows = p.rows;
     a.split = p.split;
     a.splits = p.splits;
-    a.chunk_split = p.chunk_split;
-    a.chunk_splits = p.chunk_splits;
+    a.chunk_parts = p.chunk_parts;
     a.scale = scale;
     return launched(attn_paged_launch(a, p, cache->d, dtype, cache->dtype, stream));
 }

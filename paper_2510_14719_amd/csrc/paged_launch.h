@@ -25,7 +25,9 @@ struct PagedArgs {
     int causal;
     int few_rows;                                            // sequences with more rows (new tokens x group) than this go by chunks of PAGED_CHUNK_ROWS
     int rows, split, splits;                                 // the others: rows per workgroup, keys per split (a multiple of 128), splits of the longest sequence
-    int chunk_split, chunk_splits;
+    int chunk_parts;                                         // room for partial results of chunks, in workgroups (0: chunks are not cut along the keys)
+    float *chunk_o, *chunk_ml;                               // [workgroup][PAGED_CHUNK_ROWS][d], [..][2]
+    int* chunk_what;                                         // [chunk of a key head][4]: sequence, chunk in it, pieces, workgroup of the first; behind the last [..][0] their number
     float scale;
 };
 
@@ -33,8 +35,8 @@ constexpr int PAGED_CHUNK_ROWS = 256;                        // query rows (toke
 
 // How a call is laid out (chosen by its sizes alone, so that the workspace is known beforehand).
 struct PagedPlan {
-    int few_rows, rows, split, splits, chunk_split, chunk_splits;        // as in PagedArgs
-    int tiles;                                               // workgroups of `rows` rows for a sequence; 0: all go by chunks
+    int few_rows, rows, split, splits, chunk_parts;          // as in PagedArgs
+    int waves;                                               // of a workgroup of `rows` rows: 2 or 4; 0: there is none, all sequences go by chunks
     long long chunk_tiles;                                   // chunks of all sequences, at most; 0: none does
 };
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes);

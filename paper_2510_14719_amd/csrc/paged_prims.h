@@ -37,6 +37,98 @@ __device__ __forceinline__ int seq_of_token(const int* q_start, int sequences, i
     return -1;
 }
 
+// ---- how chunks are cut along their keys
+//
+// Chunks of the sequences with more rows than few_rows are numbered through, the last one of a sequence first.  Where they are fewer than the chip has compute
+// units, those of long sequences are cut into pieces; which length to cut for is found on the device, from the lengths that are there, by every wave of the
+// kernel for itself: of 15 lengths, the longest sequence's x 2^(-c/4), the shortest that still makes no more pieces than there are compute units, if that
+// is worth the joining.  (On MI355X a tile of 64 keys takes 1.6 us, leaving partial results 6, joining them 8.  us cut / not: 12 sequences of 1 ... 777 new tokens,
+// 900 ... 4001 keys, 16 heads on 4, d 128 69 / 126; 8 of 64 new tokens, 4000 keys, the same heads 49 / 110.)
+constexpr int CHUNK_PARTS = 256;                // most pieces: a round of the compute units
+constexpr int CHUNK_UNCUT = 512;                // sequences up to this length are not cut
+constexpr float CHUNK_SAVES = 9.f, CHUNK_LEAST = 4.f;            // tiles that cutting has to save, and leaves in a piece at least
+
+struct ChunkSeq {
+    int chunks, tiles;                          // chunks of the sequence, key tiles of its longest
+};
+__device__ __forceinline__ ChunkSeq chunk_seq(const PagedArgs& a, int s)
+{
+    if (s >= a.sequences) return {0, 0};
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    const int rows = seq.n * a.group;
+    if (rows <= a.few_rows) return {0, 0};
+    return {(rows + PAGED_CHUNK_ROWS - 1) / PAGED_CHUNK_ROWS, (seq.kv + 63) / 64};
+}
+// Calls f(chunks, tiles) for every sequence that goes by chunks; `first`: those of the first 64, a lane each.
+template <typename F> __device__ __forceinline__ void each_chunk_seq(const PagedArgs& a, const ChunkSeq& first, int lane, F f)
+{
+    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+        const ChunkSeq q = s0 == 0 ? first : chunk_seq(a, s0 + lane);
+        unsigned long long there = __builtin_amdgcn_ballot_w64(q.chunks > 0);
+        while (there) {
+            const int i = __builtin_ctzll(there);
+            there &= there - 1;
+            f(__builtin_amdgcn_readlane(q.chunks, i), __builtin_amdgcn_readlane(q.tiles, i));
+        }
+    }
+}
+// Pieces of a chunk of a sequence of so many tiles, where it is cut for 1 / inverse tiles.
+__device__ __forceinline__ int chunk_pieces(float inverse, int tiles) { return max(1, (int)__builtin_ceilf((float)tiles * inverse - 0.001f)); }
+// 1 / the length to cut for (0: not at all), and how many chunks there are in that case.
+struct ChunkCut {
+    float inverse;
+    int chunks;
+};
+__device__ inline ChunkCut chunk_cut(const PagedArgs& a, const ChunkSeq& first, int key_heads, int lane)
+{
+    if (a.chunk_parts == 0) return {0.f, 0};
+    int longest = 0, chunks = 0;
+    each_chunk_seq(a, first, lane, [&](int n, int tiles) {
+        longest = max(longest, tiles);
+        chunks += n;
+    });
+    if (longest <= CHUNK_UNCUT / 64 || chunks * key_heads >= a.chunk_parts) return {0.f, 0};
+    const int c = 1 + lane % 15;
+    const float length = (float)longest * __builtin_amdgcn_exp2f(-0.25f * c), inverse = 1.f / length;
+    int pieces = 0;
+    each_chunk_seq(a, first, lane, [&](int n, int tiles) { pieces += n * chunk_pieces(inverse, tiles); });
+    const unsigned fits = (unsigned)__builtin_amdgcn_ballot_w64(lane < 15 && pieces * key_heads <= a.chunk_parts && (float)longest - length > CHUNK_SAVES && length >= CHUNK_LEAST);
+    if (fits == 0) return {0.f, 0};
+    return {__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), 31 - __builtin_clz(fits))), chunks};
+}
+// Sequence, chunk and piece with a number, and the chunk's number; s = -1 behind the last.
+struct ChunkPiece {
+    int s, chunk, piece, pieces, number;
+};
+__device__ inline ChunkPiece chunk_numbered(const PagedArgs& a, const ChunkSeq& first, float inverse, int left, int lane)
+{
+    int number = 0;
+    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+        const ChunkSeq q = s0 == 0 ? first : chunk_seq(a, s0 + lane);
+        const int pieces = chunk_pieces(inverse, q.tiles);
+        int sum = q.chunks * pieces, before = q.chunks;      // with those of the lanes before
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(sum, d), y = __shfl_up(before, d);
+            if (lane >= d) {
+                sum += x;
+                before += y;
+            }
+        }
+        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(sum > left);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond), n = __builtin_amdgcn_readlane(pieces, at), chunks = __builtin_amdgcn_readlane(q.chunks, at);
+            const int inside = left - (__builtin_amdgcn_readlane(sum, at) - chunks * n);
+            return {s0 + at, chunks - 1 - inside / n, inside % n, n, number + __builtin_amdgcn_readlane(before, at) - chunks + inside / n};
+        }
+        left -= __builtin_amdgcn_readlane(sum, 63);
+        number += __builtin_amdgcn_readlane(before, 63);
+    }
+    return {-1, 0, 0, 1, 0};
+}
+// Key tiles per piece.
+__device__ __forceinline__ int chunk_piece_tiles(int pieces, int keys) { return max(1, ((keys + 63) / 64 + pieces - 1) / pieces); }
+
 // Exchange with lane^32 and lane^16: v_permlane32_swap swaps the upper 32 lanes of its first operand with the lower 32 of its second,
 // v_permlane16_swap odd rows of 16 lanes with even ones.  (Inline asm: the compiler folds the two results of the builtins into one when
 // both inputs are the same value; the s_nop covers the VALU-write -> permlane-read hazard.)

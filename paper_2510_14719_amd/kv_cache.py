@@ -92,7 +92,14 @@ def _check(rc: int) -> None:
 def _device(x, what):
     if not x.is_cuda:
         raise ValueError("%s: device tensors are taken; got one on %s" % (what, x.device))
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError("%s: on %s, and the call goes to the current device, %d" % (what, x.device, torch.cuda.current_device()))
     return x.data_ptr()
+
+
+def _fast():
+    """The extension that makes plain calls without the interpreter's share; what it does not take (NotImplemented) goes through the code here."""
+    return binding._fast or binding._load_fast()
 
 
 def _array(x, dtype, what, shape=None):
@@ -161,6 +168,9 @@ def attn_paged(q, k_cache, v_cache, q_start, kv_len, table, o, lse, max_q, max_k
 
     ``max_q`` and ``max_kv`` bound the new tokens and the length of any sequence.  ``workspace``: a uint8 tensor of at least
     ``attn_paged_workspace`` bytes (None where that is 0)."""
+    rc = _fast().attn_paged(q, k_cache, v_cache, q_start, kv_len, table, o, lse, max_q, max_kv, scale, causal, k_scale, v_scale, workspace, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     tokens, heads, d = q.shape
     rq, ro = _rows(q, "q"), _rows(o, "o", tuple(q.shape), q.dtype)
     if d != k_cache.shape[-1]:
@@ -183,6 +193,9 @@ def rope(x, y, freq, pos=None, layout=HALF, amplitude=1.0, inverse=False, stream
 
     ``freq`` float64 [rot / 2] on the device: the first rot elements of a head are turned, the others copied.  ``pos`` int32 [batch][tokens] or
     [tokens] (None: 0, 1, ...).  ``inverse`` turns back, which is the gradient of ``x`` for a gradient of ``y``."""
+    rc = _fast().rope(x, y, freq, pos, layout, amplitude, inverse, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     if x.dim() != 4 or x.shape != y.shape or x.dtype != y.dtype:
         raise ValueError("x and y: two tensors of one type and shape [batch][heads][tokens][d]; got %s and %s" % (tuple(x.shape), tuple(y.shape)))
     _unit(x, "x")
@@ -199,6 +212,9 @@ def kv_append(k, v, k_cache, v_cache, q_start, kv_len, table, max_q, max_kv, q=N
               v_scale=None, stream=None) -> None:
     """New tokens into the cache: ``k``, ``v`` [tokens][key heads][d], K turned by its position if ``freq`` (as for ``rope``) is given, and ``q``
     [tokens][heads][d] turned into ``q_out`` beside it.  ``kv_len`` counts the new tokens already."""
+    rc = _fast().kv_append(k, v, k_cache, v_cache, q_start, kv_len, table, max_q, max_kv, q, q_out, freq, layout, amplitude, k_scale, v_scale, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     tokens = k.shape[0]
     shape = (tokens, k_cache.shape[1], k_cache.shape[3])
     rk, rv = _rows(k, "k", shape, k.dtype), _rows(v, "v", shape, k.dtype)
@@ -224,6 +240,9 @@ def _list(x, n, what):
 
 def kv_reserve(ref, table, kv_len, rows, new_len, missing, page_size, stream=None) -> None:
     """Rows get pages for ``new_len`` tokens in all, lowest free page first; ``missing`` int32 [1]: how many were not there."""
+    rc = _fast().kv_reserve(ref, table, kv_len, rows, new_len, missing, page_size, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     n = rows.numel()
     _check(_load().kv_reserve(_book(ref, table, kv_len, page_size), _list(rows, n, "rows"), _list(new_len, n, "new_len"), n, _array(missing, torch.int32, "missing"),
                               _stream(stream)))
@@ -231,12 +250,18 @@ def kv_reserve(ref, table, kv_len, rows, new_len, missing, page_size, stream=Non
 
 def kv_free(ref, table, kv_len, rows, page_size, stream=None) -> None:
     """The pages of rows are given back."""
+    rc = _fast().kv_free(ref, table, kv_len, rows, page_size, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     n = rows.numel()
     _check(_load().kv_free(_book(ref, table, kv_len, page_size), _list(rows, n, "rows"), n, _stream(stream)))
 
 
 def kv_fork(k_cache, v_cache, ref, table, kv_len, src, dst, missing, stream=None) -> None:
     """Rows ``dst`` become continuations of rows ``src``: full pages shared, a last page that is not full copied."""
+    rc = _fast().kv_fork(k_cache, v_cache, ref, table, kv_len, src, dst, missing, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     n = src.numel()
     _check(_load().kv_fork(_pages(k_cache, v_cache, layers=True), _book(ref, table, kv_len, k_cache.shape[3]), _list(src, n, "src"), _list(dst, n, "dst"), n,
                            _array(missing, torch.int32, "missing"), _stream(stream)))

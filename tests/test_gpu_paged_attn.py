@@ -228,3 +228,55 @@ def test_beside_the_contiguous_attention(kv, d, dtype):
                       workspace=workspace_for(kv, dev["q"][at:end], dev["k_cache"], 1, end - at, end))
         torch.cuda.synchronize()
         check(out, l2, [x[at:end] for x in ref], "tokens from %d" % at)
+
+
+class Sub(torch.Tensor):
+    pass
+
+
+def test_with_and_without_the_extension(kv, monkeypatch):
+    """Plain calls go through the extension, others (and all, where there is none) through the general code: the same results and the same refusals."""
+    from paper_2510_14719_amd import binding
+    assert binding._load_fast() is not binding._NoExtension
+    b = Batch([(2, 700), (1, 1100), (3, 90)], 4, 2, 64, "fp16", "e4m3", 16, pad=2)
+    results = []
+    for general in (False, True):
+        if general:
+            monkeypatch.setattr(binding, "_fast", binding._NoExtension)
+        dev = b.cuda()
+        freq, ints = kv.rope_frequencies(64).cuda(), lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        q_out = torch.zeros_like(dev["q"])
+        k = dev["q"][:, :2].clone()
+        kv.kv_append(k, k, dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], b.max_q, b.max_kv, q=dev["q"], q_out=q_out, freq=freq,
+                     layout=kv.INTERLEAVED, amplitude=1.25, **dev["scales"])
+        dev["q"] = q_out
+        call(kv, b, dev)
+        y = torch.zeros((1, 4, b.tokens, 64), dtype=torch.float16, device="cuda")
+        kv.rope(q_out.transpose(0, 1)[None], y, freq, inverse=True)
+        ref, table, kv_len, missing = torch.zeros(b.k_cache.shape[0], dtype=torch.int32, device="cuda"), dev["table"].clone(), ints(0, 0, 0), ints(9)
+        kv.kv_reserve(ref, table, kv_len, ints(0, 1), ints(100, 50), missing, 16)
+        layers = [dev[x].view(torch.uint8)[None] for x in ("k_cache", "v_cache")]
+        kv.kv_fork(*layers, ref, table, kv_len, ints(1), ints(2), missing)
+        kv.kv_free(ref, table, kv_len, ints(0), 16)
+        torch.cuda.synchronize()
+        results.append([q_out, dev["o"], dev["lse"], y, dev["k_cache"].view(torch.uint8), dev["v_cache"].view(torch.uint8), ref, table, kv_len, missing])
+        with pytest.raises(kv.KvCacheError) as e:
+            kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], None, b.max_q, b.max_kv, -1.0,
+                          workspace=torch.empty(1 << 22, dtype=torch.uint8, device="cuda"))
+        assert e.value.code == -3
+        for name, bad in (("q_start", dev["q_start"].long()), ("kv_len", dev["kv_len"][:2]), ("table", dev["table"].t()), ("o", dev["o"].float()), ("lse", dev["lse"][1:]),
+                          ("q", dev["q"][..., :32]), ("q", dev["q"].cpu()), ("k_cache", dev["k_cache"][:, :1])):
+            with pytest.raises(ValueError):
+                call(kv, b, {**dev, name: bad}, workspace=torch.empty(1 << 22, dtype=torch.uint8, device="cuda"))
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+
+
+def test_a_subclass_takes_the_general_code(kv):
+    b = Batch(FEW, 4, 2, 64, "bf16", "bf16", 16)
+    want = run(kv, b)
+    dev = b.cuda()
+    dev["q"] = dev["q"].as_subclass(Sub)
+    call(kv, b, dev)
+    torch.cuda.synchronize()
+    assert torch.equal(dev["o"], want["o"])

@@ -202,3 +202,17 @@ def test_frequencies():
     for i, bad in ((1, 0), (1, 3), (1, 1026), (2, 1.0), (2, math.inf), (2, math.nan), (3, 4), (3, -1), (4, 0.5), (4, math.nan), (5, 0.0), (5, math.inf), (6, -1.0), (7, 1.0), (7, math.inf)):
         assert lib.rope_frequencies(*ok[:i], bad, *ok[i + 1:]) == SHAPE, (i, bad)
     assert lib.rope_frequencies(buf, 2, 1e4, 2, 4.0, 0.0, 0.0, 0.0) == SHAPE
+
+
+def test_what_the_extension_does_not_take():
+    """CPU tensors, other counts of arguments and other types are left, untouched, to the general code."""
+    from paper_2510_14719_amd import binding
+    fast = binding._load_fast()
+    x = torch.zeros((3, 2, 64), dtype=torch.float16)
+    for f, n in ((fast.attn_paged, 16), (fast.kv_append, 17), (fast.rope, 8), (fast.kv_reserve, 8), (fast.kv_free, 6), (fast.kv_fork, 9)):
+        for args in ([x] * n, [None] * n, [1] * n, [], [x] * (n + 1)):
+            assert f(*args) is NotImplemented
+    with pytest.raises(TypeError):
+        fast.bind_kv(1)
+    with pytest.raises(ValueError):
+        fast.bind_kv(0, 0, 0, 0, 0, 0)

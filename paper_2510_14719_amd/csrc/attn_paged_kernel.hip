@@ -19,8 +19,9 @@ namespace {
 
 // The softmax reference moves only when a row maximum grew by more than this many powers of two.
 constexpr float MOVE_LOG2 = 8.0f;
+constexpr int NW = 4;                           // waves of a workgroup
 
-template <int D, int ES, int QB, int NW> struct FewLayout {
+template <int D, int ES, int QB> struct FewLayout {
     typedef CachedRows<D, ES, 32> Rows;
     static constexpr int STAGE = 2 * Rows::BYTES, SLOTS = 2, RING = NW * SLOTS * STAGE;
     static constexpr int JOIN = NW * (D / 16) * QB * 1024;   // O of every wave
@@ -28,12 +29,12 @@ template <int D, int ES, int QB, int NW> struct FewLayout {
     static constexpr int SMEM = (RING > JOIN ? RING : JOIN) + SUMS;
 };
 
-template <int DTYPE, bool C8, int D, int QB, int NW>
+template <int DTYPE, bool C8, int D, int QB>
 __global__ __launch_bounds__(NW * 64)
 void attn_paged_few(PagedArgs a)
 {
     typedef Elem<DTYPE> E;
-    typedef FewLayout<D, C8 ? 1 : 2, QB, NW> Layout;
+    typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
     typedef typename Layout::Rows Rows;
     constexpr int KK = D / 32, FB = D / 16, ROWS = QB * 16;
     constexpr int SUBS = 16 / Rows::PER_PIECE;               // pieces of 16 keys and a line of their rows
@@ -46,20 +47,20 @@ void attn_paged_few(PagedArgs a)
     const int h = id % key_heads;
     id /= key_heads;
     const int sp = id % a.splits, s = id / a.splits;
-    // ---- the wave's steps are 32 keys each, every NW-th of the split's.  Their table entries are asked for before the sequence's length is known.
-    const int k0 = sp * a.split;
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    if (seq.n == 0 || seq.n * a.group > a.few_rows) return;
+    const int keys = paged_tile_keys(0, ROWS, seq.n, a.group, seq.kv, a.causal), per = paged_piece_keys(keys, a.split);
+    const int k0 = sp * per, k1 = min(keys, k0 + per);
+    if (sp > 0 && k0 >= keys) return;
+    const bool whole = keys <= per;
+
+    // ---- the wave's steps are 32 keys each, every NW-th of the piece's
     const int* const table = a.table + (long long)s * a.table_stride;
     auto entries_of = [&](int step) __attribute__((always_inline)) {     // lane 2 i + hf: page of half hf of the i-th step from here
-        const int key = min(k0 + ((step + (lane >> 1)) * NW + wave) * 32 + (lane & 1) * 16, a.max_kv - 1);
+        const int key = max(min(k0 + ((step + (lane >> 1)) * NW + wave) * 32 + (lane & 1) * 16, keys - 1), 0);
         return table[key >> a.page_shift];
     };
     int entries = entries_of(0);
-    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-    if (seq.n == 0 || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(0, ROWS, seq.n, a.group, seq.kv, a.causal);
-    const int k1 = min(keys, k0 + a.split);
-    if (sp > 0 && k0 >= keys) return;
-    const bool whole = keys <= a.split;
 
     // ---- rows: lane % 16 of each 16-row block
     s16x8 Qf[QB][KK];
@@ -319,8 +320,9 @@ void attn_paged_join(PagedArgs a)
     const SeqRange seq = seq_range(a.q_start, a.kv_len, blockIdx.x / most / key_heads, a.tokens, a.max_q, a.max_kv);
     if (r >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
     const int keys = paged_tile_keys(0, a.rows, seq.n, a.group, seq.kv, a.causal);
-    if (keys <= a.split) return;
-    const int n = (keys + a.split - 1) / a.split, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
+    const int per = paged_piece_keys(keys, a.split);
+    if (keys <= per) return;
+    const int n = (keys + per - 1) / per, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
     const long long row = (long long)t * a.heads + head, all = (long long)a.tokens * a.heads;
     const float* const part_o = a.part_o + row * D;
     const float* const part_ml = a.part_ml + row * 2;
@@ -387,11 +389,11 @@ void attn_paged_join_chunks(PagedArgs a)
     if (a.lse && e == 0) a.lse[(long long)t * a.heads + head] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <int DTYPE, bool C8, int D, int QB, int NW>
+template <int DTYPE, bool C8, int D, int QB>
 int launch_few(const PagedArgs& a, hipStream_t stream)
 {
-    typedef FewLayout<D, C8 ? 1 : 2, QB, NW> Layout;
-    auto kern = attn_paged_few<DTYPE, C8, D, QB, NW>;
+    typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
+    auto kern = attn_paged_few<DTYPE, C8, D, QB>;
     static PerDeviceOnce once;
     if (once.prepare(reinterpret_cast<const void*>(kern), Layout::SMEM) < 0) return -1;
     PagedArgs arg = a;
@@ -404,8 +406,7 @@ template <int DTYPE, bool C8, int D>
 int launch_all(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 {
     int rc = 0;
-    if (plan.waves == 4) rc = plan.rows == 16 ? launch_few<DTYPE, C8, D, 1, 4>(a, stream) : launch_few<DTYPE, C8, D, 2, 4>(a, stream);
-    if (plan.waves == 2) rc = plan.rows == 16 ? launch_few<DTYPE, C8, D, 1, 2>(a, stream) : launch_few<DTYPE, C8, D, 2, 2>(a, stream);
+    if (plan.few_rows > 0) rc = plan.rows == 16 ? launch_few<DTYPE, C8, D, 1>(a, stream) : launch_few<DTYPE, C8, D, 2>(a, stream);
     if (rc == 0 && plan.chunk_tiles > 0) rc = attn_paged_chunk_launch(a, plan, D, DTYPE, C8 ? KV_E4M3 : DTYPE, stream);
     PagedArgs arg = a;
     void* args[] = {&arg};
@@ -433,13 +434,18 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
     p.rows = most <= 16 ? 16 : 32;
     p.few_rows = most <= 32 || (long long)sequences * key_heads > 64 ? 32 : 0;
     if (p.few_rows) {
-        const long long units = (long long)sequences * key_heads, most_keys = (768 << 10) / (2 * d * cache_bytes);
-        long long split = units >= 512 ? most_keys : (units * max_kv / 1024 + 127) / 128 * 128;
-        if (split > most_keys) split = most_keys;
+        // Pieces: about one for every workgroup that the chip holds (one a compute unit with rows of 256 bytes, two with 128, four with 64), of 512 keys at least;
+        // where there are 512 workgroups or more anyway, pieces only serve to even out lengths, and have 1.25 MiB of keys and values.  A piece
+        // costs 4 us besides its keys, the joining 6.  us at most keys of a piece 512 / 768 / 1536 / 2560 / 4096, d 128, 32 heads on 8:
+        // 64 sequences of 4000 218 / 211 / 197 / 191 / 183; of 300 ... 16384 260 / 232 / 211 / 211 / 251; one of 32768 35 / 38 / 31 / 37 / 49;
+        // one of 2000 13 / 15 / 17 / 22 (whole); 8 of 900, whole 15.
+        const long long units = (long long)sequences * key_heads, key_bytes = 2ll * d * cache_bytes;
+        const long long even = (5 << 18) / key_bytes, chip = 256 * (512 / key_bytes);
+        long long split = units >= 512 ? even : units * max_kv / chip;
         if (split < 512) split = 512;
-        if (max_kv > 1024 && split < whole) p.split = (int)split;
+        if (max_kv <= (units >= 512 ? even * 8 / 5 : 1024)) split = whole;
+        if (split < whole) p.split = (int)((split + 127) / 128 * 128);
         p.splits = (int)((max_kv + p.split - 1) / p.split);
-        p.waves = units * p.splits <= 256 ? 4 : 2;
     }
     if (most > 32) {
         const long long each = (most + PAGED_CHUNK_ROWS - 1) / PAGED_CHUNK_ROWS * sequences, all = (long long)tokens * group / PAGED_CHUNK_ROWS + sequences;

@@ -24,7 +24,7 @@ struct PagedArgs {
     int heads, group;                                        // query heads, and how many share a key head
     int causal;
     int few_rows;                                            // sequences with more rows (new tokens x group) than this go by chunks of PAGED_CHUNK_ROWS
-    int rows, split, splits;                                 // the others: rows per workgroup, keys per split (a multiple of 128), splits of the longest sequence
+    int rows, split, splits;                                 // the others: rows per workgroup, most keys of a piece (a multiple of 128), pieces of the longest sequence
     int chunk_parts;                                         // room for partial results of chunks, in workgroups (0: chunks are not cut along the keys)
     float *chunk_o, *chunk_ml;                               // [workgroup][PAGED_CHUNK_ROWS][d], [..][2]
     int* chunk_what;                                         // [chunk of a key head][4]: sequence, chunk in it, pieces, workgroup of the first; behind the last [..][0] their number
@@ -35,8 +35,7 @@ constexpr int PAGED_CHUNK_ROWS = 256;                        // query rows (toke
 
 // How a call is laid out (chosen by its sizes alone, so that the workspace is known beforehand).
 struct PagedPlan {
-    int few_rows, rows, split, splits, chunk_parts;          // as in PagedArgs
-    int waves;                                               // of a workgroup of `rows` rows: 2 or 4; 0: there is none, all sequences go by chunks
+    int few_rows, rows, split, splits, chunk_parts;          // as in PagedArgs (few_rows 0: all sequences go by chunks)
     long long chunk_tiles;                                   // chunks of all sequences, at most; 0: none does
 };
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes);
@@ -54,6 +53,14 @@ PAGED_HD inline int paged_tile_keys(int tile, int rows, int n, int group, int kv
 // Enqueue for validated arguments: 0, or -1 if HIP refused a launch.
 int attn_paged_chunk_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream);
 int attn_paged_launch(const PagedArgs& a, const PagedPlan& plan, int d, int dtype, int cache_dtype, void* stream);
+
+// Keys of a piece where a row of so many keys is cut into as many pieces as it has splits begun, all alike (the last may be shorter, or there are fewer).
+PAGED_HD inline int paged_piece_keys(int keys, int split)
+{
+    if (keys <= split) return split;
+    const int n = (keys + split - 1) / split;
+    return ((keys + n - 1) / n + 63) / 64 * 64;
+}
 
 struct RopeArgs {
     const char* x;

@@ -101,59 +101,61 @@ void attn_paged_chunk(PagedArgs a)
     const int group = PPW == 4 ? wave >> 2 : 0;
     constexpr int SUBS = PPW == 4 ? 2 : 1;                   // pieces of K (and of V)
     const int sub0 = PPW == 2 ? wave & 1 : 0;
-    unsigned k_off[SUBS], v_off[SUBS];
-    int piece_row[SUBS];                                     // of the lane, inside the 16 keys
+    unsigned k_off[SUBS], v_off[SUBS];                       // source offsets of the lane inside 16 whole rows
+    int piece_row[SUBS];                                     // row of the lane among the 16
 #pragma unroll
     for (int i = 0; i < SUBS; ++i) {
         const int r = (sub0 + i) * Rows::PER_PIECE + lane / Rows::COLS, col = lane % Rows::COLS;
         piece_row[i] = r;
-        k_off[i] = (unsigned)((col ^ Rows::sw_k(block * 16 + r)) * 16 + group * 128);
-        v_off[i] = (unsigned)((col ^ Rows::sw_v(block * 16 + r)) * 16 + group * 128);
+        k_off[i] = (unsigned)((col ^ Rows::sw_k(block * 16 + r)) * 16 + group * 128) + r * (unsigned)a.token_bytes;
+        v_off[i] = (unsigned)((col ^ Rows::sw_v(block * 16 + r)) * 16 + group * 128) + r * (unsigned)a.token_bytes;
     }
     const unsigned lds = (unsigned)(size_t)(LDS_AS void*)smem;
     const int to0 = group * (BN * Rows::LINE) + (block * 16 + sub0 * Rows::PER_PIECE) * Rows::LINE;
-    const char* const kh = uniform_ptr(a.k + h * a.head_bytes);
-    const char* const vh = uniform_ptr(a.v + h * a.head_bytes);
     const int* const table = a.table + (long long)s * a.table_stride;
     const int page_mask = (1 << a.page_shift) - 1, token_bytes = (int)a.token_bytes;
-    int entries = 0;                            // lane i: page of this wave's block of tile i of the current 64
+    const long long k_base = reinterpret_cast<long long>(uniform_ptr(a.k + h * a.head_bytes)), v_minus_k = reinterpret_cast<long long>(uniform_ptr(a.v)) - reinterpret_cast<long long>(uniform_ptr(a.k));
+    const int inside = __builtin_amdgcn_readfirstlane(keys - 16 - block * 16 - k0 < 0 ? 0 : (keys - 16 - block * 16 - k0) / BN + 1);   // tiles whose 16 keys all exist
+    // Lane i: where the first of this wave's keys of tile i of the current 64 stands in K.  (Addresses are worked out for 64 tiles at a time: with every tile for itself a
+    // wave was held 500 cycles by its copies, of 3100 a tile; 4096 new tokens of 16384, 32 heads on 8, d 128: 769 us that way, 753 so.)
+    unsigned place_lo = 0, place_hi = 0;
     bool any_bad = false;                       // a page of the tiles so far is none
-    int page_k = 0, page_v = 0;
-    auto load_entries = [&](int t0) __attribute__((always_inline)) {
-        const int key = k0 + (t0 + lane) * BN;
+    auto load_places = [&](int t0) __attribute__((always_inline)) {
+        const int key = k0 + (t0 + lane) * BN, first_key = min(key + block * 16, keys - 1);
         bool bad = false;
 #pragma unroll
         for (int b = 0; b < KB; ++b) bad |= (unsigned)table[min(key + b * 16, keys - 1) >> a.page_shift] >= (unsigned)a.pages;
-        entries = table[min(key + block * 16, keys - 1) >> a.page_shift];
         any_bad |= __builtin_amdgcn_ballot_w64(bad) != 0;
+        int page = table[first_key >> a.page_shift];
+        page = (unsigned)page < (unsigned)a.pages ? page : 0;
+        const unsigned long long place = k_base + page * a.page_bytes + (first_key & page_mask) * token_bytes;
+        place_lo = (unsigned)place;
+        place_hi = (unsigned)(place >> 32);
     };
-    auto copy_tile = [&](const char* base, int page, int t, const unsigned (&off)[SUBS], unsigned dst) __attribute__((always_inline)) {
-        const int key = k0 + t * BN + block * 16;
-        const char* const at = base + page * a.page_bytes;
-        if (key + 16 <= keys) {
-            const char* const from = at + (key & page_mask) * token_bytes;
+    unsigned long long place_k = 0, place_v = 0;             // of the K tile of the stage; in K too, of its V tile
+    auto copy_tile = [&](unsigned long long place, int t, const unsigned (&off)[SUBS], unsigned dst) __attribute__((always_inline)) {
+        if (t < inside) {
 #pragma unroll
-            for (int i = 0; i < SUBS; ++i) dma16(from, off[i] + piece_row[i] * token_bytes, dst + i * (Rows::PER_PIECE * Rows::LINE));
+            for (int i = 0; i < SUBS; ++i) dma16(reinterpret_cast<const void*>(place), off[i], dst + i * (Rows::PER_PIECE * Rows::LINE));
         } else {                                // rows behind the last key: that one again (they are masked, or never read)
+            const int key = k0 + min(t, nt - 1) * BN + block * 16;
+            const char* const page = reinterpret_cast<const char*>(place) - (min(key, keys - 1) & page_mask) * token_bytes;
 #pragma unroll
             for (int i = 0; i < SUBS; ++i)
-                dma16(at, off[i] + (min(key + piece_row[i], keys - 1) & page_mask) * token_bytes, dst + i * (Rows::PER_PIECE * Rows::LINE));
+                dma16(page, off[i] + (unsigned)(((min(key + piece_row[i], keys - 1) & page_mask) - piece_row[i]) * token_bytes), dst + i * (Rows::PER_PIECE * Rows::LINE));
         }
     };
     auto issue_stage = [&](int st) __attribute__((always_inline)) {      // in order, from -1 on
         const unsigned dst = lds + ((st + STAGES) % STAGES) * STAGE + to0;
         const int t = st + 1;
+        place_v = place_k;
         if (t < nt) {
-            if ((t & 63) == 0) load_entries(t);
-            const int page = __builtin_amdgcn_readlane(entries, t & 63);
-            page_v = page_k;
-            page_k = (unsigned)page < (unsigned)a.pages ? page : 0;
-        } else {
-            page_v = page_k;
+            if ((t & 63) == 0) load_places(t);
+            place_k = (unsigned)__builtin_amdgcn_readlane(place_lo, t & 63) | (unsigned long long)(unsigned)__builtin_amdgcn_readlane(place_hi, t & 63) << 32;
         }
         // (behind the last tile, and before the first, something is copied all the same: the waits count copies)
-        if (copies_k) copy_tile(kh, page_k, min(t, nt - 1), k_off, dst);
-        if (copies_v) copy_tile(vh, t == 0 ? page_k : page_v, max(st, 0), v_off, dst + Rows::BYTES);
+        if (copies_k) copy_tile(place_k, t, k_off, dst);
+        if (copies_v) copy_tile((t == 0 ? place_k : place_v) + v_minus_k, max(st, 0), v_off, dst + Rows::BYTES);
     };
     auto wait_stage = [&](int j) __attribute__((always_inline)) {
         if (j + 1 < nt) wait_vmcnt<PPW>(); else wait_vmcnt<0>();

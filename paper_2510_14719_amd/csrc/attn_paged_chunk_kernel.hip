@@ -31,10 +31,11 @@ __global__ __launch_bounds__(NW * 64)
 void attn_paged_chunk(PagedArgs a)
 {
     typedef Elem<DTYPE> E;
-    typedef CachedRows<D, C8 ? 1 : 2, BN> Rows;
+    typedef CachedRows<D, 2, BN> Rows;                       // in the LDS: 16-bit values, whatever the cache holds
     constexpr int KK = D / 32, FB = D / 16, STAGE = 2 * Rows::BYTES;
-    constexpr int PIECES = Rows::BYTES / 1024;               // copies of a K or V tile
-    constexpr int PPW = 2 * PIECES / NW;                     // copies of a stage that a wave issues: 4 (K, K, V, V), 2 (K, V) or 1
+    constexpr int COLS = D * (C8 ? 1 : 2) / 16 < 8 ? D * (C8 ? 1 : 2) / 16 : 8;          // 16-byte columns of a cached row that a copy takes
+    constexpr int PER_PIECE = 64 / COLS;                     // rows of a copy of 64 x 16 bytes
+    constexpr int PPW = 2 * BN * D * (C8 ? 1 : 2) / 1024 / NW;           // copies of a stage that a wave issues: 4 (K, K, V, V), 2 (K, V) or 1
     extern __shared__ __attribute__((aligned(1024))) char smem[];
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lc = lane & 15, lg = lane >> 4;
@@ -105,13 +106,13 @@ void attn_paged_chunk(PagedArgs a)
     int piece_row[SUBS];                                     // row of the lane among the 16
 #pragma unroll
     for (int i = 0; i < SUBS; ++i) {
-        const int r = (sub0 + i) * Rows::PER_PIECE + lane / Rows::COLS, col = lane % Rows::COLS;
+        const int r = (sub0 + i) * PER_PIECE + lane / COLS, col = lane % COLS;
         piece_row[i] = r;
-        k_off[i] = (unsigned)((col ^ Rows::sw_k(block * 16 + r)) * 16 + group * 128) + r * (unsigned)a.token_bytes;
-        v_off[i] = (unsigned)((col ^ Rows::sw_v(block * 16 + r)) * 16 + group * 128) + r * (unsigned)a.token_bytes;
+        k_off[i] = (unsigned)((C8 ? col : col ^ Rows::sw_k(block * 16 + r)) * 16 + group * 128) + r * (unsigned)a.token_bytes;
+        v_off[i] = (unsigned)((C8 ? col : col ^ Rows::sw_v(block * 16 + r)) * 16 + group * 128) + r * (unsigned)a.token_bytes;
     }
     const unsigned lds = (unsigned)(size_t)(LDS_AS void*)smem;
-    const int to0 = group * (BN * Rows::LINE) + (block * 16 + sub0 * Rows::PER_PIECE) * Rows::LINE;
+    const int to0 = group * (BN * Rows::LINE) + (block * 16 + sub0 * PER_PIECE) * Rows::LINE;
     const int* const table = a.table + (long long)s * a.table_stride;
     const int page_mask = (1 << a.page_shift) - 1, token_bytes = (int)a.token_bytes;
     const long long k_base = reinterpret_cast<long long>(uniform_ptr(a.k + h * a.head_bytes)), v_minus_k = reinterpret_cast<long long>(uniform_ptr(a.v)) - reinterpret_cast<long long>(uniform_ptr(a.k));
@@ -133,33 +134,88 @@ void attn_paged_chunk(PagedArgs a)
         place_hi = (unsigned)(place >> 32);
     };
     unsigned long long place_k = 0, place_v = 0;             // of the K tile of the stage; in K too, of its V tile
-    auto copy_tile = [&](unsigned long long place, int t, const unsigned (&off)[SUBS], unsigned dst) __attribute__((always_inline)) {
-        if (t < inside) {
-#pragma unroll
-            for (int i = 0; i < SUBS; ++i) dma16(reinterpret_cast<const void*>(place), off[i], dst + i * (Rows::PER_PIECE * Rows::LINE));
-        } else {                                // rows behind the last key: that one again (they are masked, or never read)
+    // Where the lane's 16 bytes of piece i stand, in tile t of K or V (rows behind the last key: that one again; they are masked, or never read).
+    auto source = [&](unsigned long long place, int t, const unsigned (&off)[SUBS], int i, unsigned& lane_off) __attribute__((always_inline)) -> const char* {
+        lane_off = off[i];
+        const char* base = reinterpret_cast<const char*>(place);
+        if (t >= inside) {
             const int key = k0 + min(t, nt - 1) * BN + block * 16;
-            const char* const page = reinterpret_cast<const char*>(place) - (min(key, keys - 1) & page_mask) * token_bytes;
-#pragma unroll
-            for (int i = 0; i < SUBS; ++i)
-                dma16(page, off[i] + (unsigned)(((min(key + piece_row[i], keys - 1) & page_mask) - piece_row[i]) * token_bytes), dst + i * (Rows::PER_PIECE * Rows::LINE));
+            base -= (min(key, keys - 1) & page_mask) * token_bytes;
+            lane_off += (unsigned)(((min(key + piece_row[i], keys - 1) & page_mask) - piece_row[i]) * token_bytes);
         }
+        return base;
     };
-    auto issue_stage = [&](int st) __attribute__((always_inline)) {      // in order, from -1 on
-        const unsigned dst = lds + ((st + STAGES) % STAGES) * STAGE + to0;
+    // Moves on to the K tile of stage st (in order, from -1 on) and the V tile of the same stage.
+    auto advance = [&](int st) __attribute__((always_inline)) {
         const int t = st + 1;
         place_v = place_k;
         if (t < nt) {
             if ((t & 63) == 0) load_places(t);
             place_k = (unsigned)__builtin_amdgcn_readlane(place_lo, t & 63) | (unsigned long long)(unsigned)__builtin_amdgcn_readlane(place_hi, t & 63) << 32;
         }
-        // (behind the last tile, and before the first, something is copied all the same: the waits count copies)
-        if (copies_k) copy_tile(place_k, t, k_off, dst);
-        if (copies_v) copy_tile((t == 0 ? place_k : place_v) + v_minus_k, max(st, 0), v_off, dst + Rows::BYTES);
     };
+    // A 16-bit cache: straight into the LDS.
+    auto issue_stage = [&](int st) __attribute__((always_inline)) {
+        advance(st);
+        const unsigned dst = lds + ((st + STAGES) % STAGES) * STAGE + to0;
+        // (behind the last tile, and before the first, something is copied all the same: the waits count copies)
+#pragma unroll
+        for (int i = 0; i < SUBS; ++i) {
+            unsigned off;
+            const char* const from = source(place_k, st + 1, k_off, i, off);
+            dma16(from, off, dst + i * (PER_PIECE * Rows::LINE));
+        }
+#pragma unroll
+        for (int i = 0; i < SUBS; ++i) {
+            unsigned off;
+            const char* const from = source((st < 0 ? place_k : place_v) + v_minus_k, max(st, 0), v_off, i, off);
+            dma16(from, off, dst + Rows::BYTES + i * (PER_PIECE * Rows::LINE));
+        }
+    };
+    // An 8-bit cache: into registers a stage ahead, widened once and written to the LDS (widened by every wave as it reads, the same values take the vector ALU longer
+    // than the products take the matrix cores: 4096 new tokens of 16384, 32 heads on 8, d 128: 1015 us that way, 848 so).
+    u32x4 raw_k, raw_v;
+    auto fetch_stage = [&](int st) __attribute__((always_inline)) {
+        advance(st);
+        unsigned off;
+        if (copies_k) {
+            const char* const from = source(place_k, st + 1, k_off, 0, off);
+            raw_k = *reinterpret_cast<const u32x4*>(from + off);
+        }
+        if (copies_v) {
+            const char* const from = source((st < 0 ? place_k : place_v) + v_minus_k, max(st, 0), v_off, 0, off);
+            raw_v = *reinterpret_cast<const u32x4*>(from + off);
+        }
+    };
+    auto write_stage = [&](int st) __attribute__((always_inline)) {
+        char* const dst = smem + ((st + STAGES) % STAGES) * STAGE;
+        const int r = block * 16 + piece_row[0], byte = lane % COLS * 32, line = byte / Rows::LINE, col = byte % Rows::LINE / 16;
+        char* const to = dst + line * (BN * Rows::LINE) + r * Rows::LINE;
+        if (copies_k) {
+            *reinterpret_cast<s16x8*>(to + (col ^ Rows::sw_k(r)) * 16) = widen8<DTYPE>(u32x2{raw_k[0], raw_k[1]});
+            *reinterpret_cast<s16x8*>(to + ((col + 1) ^ Rows::sw_k(r)) * 16) = widen8<DTYPE>(u32x2{raw_k[2], raw_k[3]});
+        }
+        if (copies_v) {
+            *reinterpret_cast<s16x8*>(to + Rows::BYTES + (col ^ Rows::sw_v(r)) * 16) = widen8<DTYPE>(u32x2{raw_v[0], raw_v[1]});
+            *reinterpret_cast<s16x8*>(to + Rows::BYTES + ((col + 1) ^ Rows::sw_v(r)) * 16) = widen8<DTYPE>(u32x2{raw_v[2], raw_v[3]});
+        }
+    };
+    // At barrier j every wave's share of stages <= j has landed (8 bits: of stages <= j + 1) and nobody reads stage j - 2 any more, so that stage takes
+    // stage j + 2.
     auto wait_stage = [&](int j) __attribute__((always_inline)) {
-        if (j + 1 < nt) wait_vmcnt<PPW>(); else wait_vmcnt<0>();
+        if (C8) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        else if (j + 1 < nt) wait_vmcnt<PPW>();
+        else wait_vmcnt<0>();
         __builtin_amdgcn_s_barrier();
+    };
+    auto next = [&](int j) __attribute__((always_inline)) {
+        if (j + 2 >= nt) return;
+        if constexpr (C8) {
+            write_stage(j + 2);
+            if (j + 3 < nt) fetch_stage(j + 3);
+        } else {
+            issue_stage(j + 2);
+        }
     };
     auto stage_ptr = [&](int st) __attribute__((always_inline)) -> const char* { return smem + ((st + STAGES) % STAGES) * STAGE; };
 
@@ -299,18 +355,27 @@ void attn_paged_chunk(PagedArgs a)
     constexpr std::true_type YES{};
     constexpr std::false_type NO{};
     if (nt > 0) {
-        issue_stage(-1);
-        issue_stage(0);
-        issue_stage(1);
+#pragma unroll
+        for (int st = -1; st < 2; ++st) {
+            if constexpr (C8) {
+                fetch_stage(st);
+                write_stage(st);
+            } else {
+                issue_stage(st);
+            }
+        }
+        if constexpr (C8) {
+            if (2 < nt) fetch_stage(2);
+        }
     }
     // (Q is used once here, so that the compiler waits for its loads before the loop, and with them for the copies)
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) asm volatile("" :: "v"(Qf[qb][kk]));
-    wait_vmcnt<0>();
+    if (C8) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    else wait_vmcnt<0>();
     __builtin_amdgcn_s_barrier();
-    auto next = [&](int j) __attribute__((always_inline)) { if (j + 2 < nt) issue_stage(j + 2); };
     // (the last tile of a wave is none of these: it is always done with care)
     auto whole_tiles = [&](int j) __attribute__((always_inline)) { return j < nt_full && j + 1 < nt_w && !any_bad; };
     if (nt_w == 0) {                            // no row of this wave sees a key of the split: it only copies
@@ -394,7 +459,7 @@ void attn_paged_chunk(PagedArgs a)
 template <int DTYPE, bool C8, int D>
 int launch(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 {
-    constexpr int SMEM = STAGES * 2 * CachedRows<D, C8 ? 1 : 2, BN>::BYTES;
+    constexpr int SMEM = STAGES * 2 * CachedRows<D, 2, BN>::BYTES;
     auto kern = attn_paged_chunk<DTYPE, C8, D>;
     static PerDeviceOnce once;
     if (once.prepare(reinterpret_cast<const void*>(kern), SMEM) < 0) return -1;

@@ -172,8 +172,10 @@ int check_copy(const kv_pages* c)
 PageCopy copy_of(const kv_pages* c)
 {
     const int es = c->dtype == KV_E4M3 ? 1 : 2;
+    const i64 d = c->d, ts = c->page_size > 1 ? c->token_stride : d, hs = c->heads > 1 ? c->head_stride : d * c->page_size;
+    const bool solid = (ts == d && hs == d * c->page_size) || (hs == d && ts == d * c->heads) || (c->heads == 1 && ts == d);
     return {(char*)c->k, (char*)c->v, c->layer_stride * es, c->page_stride * es, c->head_stride * es, c->token_stride * es,
-            c->layers, c->pages, c->heads, c->page_size, c->d * es};
+            c->layers, c->pages, c->heads, c->page_size, c->d * es, solid};
 }
 bool same_pages(const kv_pages* c, const kv_book* b) { return c->pages == b->pages && c->page_size == b->page_size; }
 int launched(int rc) { return rc == 0 ? KV_OK : KV_ERR_LAUNCH; }

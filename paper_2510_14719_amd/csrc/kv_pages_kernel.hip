@@ -136,18 +136,32 @@ void free_kernel(kv_book b, const int* list)
     if (threadIdx.x == 0) b.kv_len[r] = 0;
 }
 
-// A page's contents by a workgroup: rows of 16-byte chunks, part `part` of `parts`.
+// Part `part` of `parts` of a page's contents by a workgroup, 16 bytes a lane, UNROLL of them under way (256 pages of 1 MiB in 8 layers moving together, 525 MB read and
+// written: 120 / 119 / 118 / 115 us with 1 / 2 / 4 / 8).
+constexpr int UNROLL = 8;
 __device__ __forceinline__ void copy_page(const PageCopy& c, char* base, int layer, long long src, long long dst, int part, int parts)
 {
-    const int cols = c.row_bytes / 16, all = c.heads * c.page_size * cols;   // (powers of two but for the heads)
+    const int cols = c.row_bytes / 16, all = c.heads * c.page_size * cols, per = (all + parts - 1) / parts, end = min(all, (part + 1) * per);
     const char* const from = base + layer * c.layer + src * c.page;
     char* const to = base + layer * c.layer + dst * c.page;
     const bool heads_inside = c.head < c.token;
-    for (int i = part * 256 + threadIdx.x; i < all; i += parts * 256) {
-        const int col = i % cols, r = i / cols;
-        const int h = heads_inside ? r % c.heads : r / c.page_size, t = heads_inside ? r / c.heads : r % c.page_size;
-        const long long at = h * c.head + t * c.token + col * 16;
-        *reinterpret_cast<u32x4*>(to + at) = *reinterpret_cast<const u32x4*>(from + at);
+    for (int i0 = part * per + threadIdx.x; i0 < end; i0 += 256 * UNROLL) {
+        long long at[UNROLL];
+        u32x4 w[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int i = min(i0 + u * 256, end - 1);
+            if (c.solid) {
+                at[u] = i * 16ll;
+            } else {
+                const int col = i % cols, r = i / cols, h = heads_inside ? r % c.heads : r / c.page_size, t = heads_inside ? r / c.heads : r % c.page_size;
+                at[u] = h * c.head + t * c.token + col * 16;
+            }
+            w[u] = *reinterpret_cast<const u32x4*>(from + at[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (i0 + u * 256 < end) *reinterpret_cast<u32x4*>(to + at[u]) = w[u];
     }
 }
 

@@ -93,6 +93,7 @@ struct PageCopy {
     char *k, *v;
     long long layer, page, head, token;
     int layers, pages, heads, page_size, row_bytes;
+    bool solid;                                              // the rows of a page of a layer lie without gaps, in whatever order
 };
 int kv_reserve_launch(const kv_book& b, const int* list, const int* new_len, int n, int* missing, void* stream);
 int kv_free_launch(const kv_book& b, const int* list, int n, void* stream);

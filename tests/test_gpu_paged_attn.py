@@ -69,6 +69,31 @@ def test_a_long_chunk(kv, dtype, cache):
     run(kv, Batch([(513, 513), (2, 600)], 2, 1, 64, dtype, cache, 64), what="chunk of 513")
 
 
+@pytest.mark.parametrize("G,Hk,dtype,cache", [(4, 1, "bf16", "bf16"), (2, 2, "fp16", "e4m3")])
+def test_many_sequences_of_all_kinds(kv, G, Hk, dtype, cache):
+    """More than a wave has lanes: single tokens, none at all, and chunks that are cut along their keys between them."""
+    lens = [((1, 3, 0, 5, 1)[i % 5], 8 + 7 * i % 90) for i in range(150)]
+    for i, long in ((3, (40, 1500)), (64, (20, 900)), (70, (70, 70)), (127, (9, 1100)), (149, (33, 700))):
+        lens[i] = long
+    run(kv, Batch(lens, G * Hk, Hk, 64, dtype, cache, 16, pad=5))
+
+
+def test_two_calls_at_once(kv):
+    """On two streams, each with a workspace of its own."""
+    b = Batch([(1, 3000), (2, 2100), (40, 1300)], 4, 2, 128, "bf16", "bf16", 16)
+    want = run(kv, b)
+    devs, streams = [b.cuda() for _ in "ab"], [torch.cuda.Stream() for _ in "ab"]
+    ws = [workspace_for(kv, d["q"], d["k_cache"], 3, b.max_q, b.max_kv) for d in devs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for dev, stream, w in zip(devs, streams, ws):
+            with torch.cuda.stream(stream):
+                call(kv, b, dev, workspace=w)
+    torch.cuda.synchronize()
+    for dev in devs:
+        assert torch.equal(dev["o"], want["o"]) and torch.equal(dev["lse"], want["lse"])
+
+
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 def test_rows_that_see_nothing(kv, cache):
     # sequences without new tokens, without keys, with more new tokens than keys, in pages that are none

@@ -65,6 +65,16 @@ def test_rope_and_its_gradient(kv, B, H, N, d, rot, layout):
         assert torch.equal(view.contiguous(), y) and bool((packed[:, :, 0] == 9).all()) and bool((packed[:, :, -1] == 9).all())
 
 
+def test_many_tokens_with_long_heads(kv):
+    """The most sines and cosines that a workgroup keeps."""
+    x = torch.randn((1, 1, 16389, 1024), generator=torch.Generator().manual_seed(2)).half()
+    f = kv.rope_frequencies(1024)
+    y = torch.full_like(x, float("nan"), device="cuda")
+    kv.rope(x.cuda(), y, f.cuda(), layout=kv.INTERLEAVED)
+    want, bound = turned(x.double(), torch.arange(16389).expand(1, 1, 16389), f, 1)
+    near(y, want, bound, torch.float16)
+
+
 def test_positions_by_default_and_shared(kv):
     x = torch.randn((3, 2, 50, 64), generator=torch.Generator().manual_seed(3)).half().cuda()
     f = kv.rope_frequencies(64).cuda()

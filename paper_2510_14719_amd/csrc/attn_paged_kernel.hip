@@ -209,24 +209,24 @@ void attn_paged_few(PagedArgs a)
 #pragma unroll
             for (int t = 0; t < 4; ++t) P[qb][t] = E::pack2(S[t / 2][qb][t % 2 * 2], S[t / 2][qb][t % 2 * 2 + 1]);
         }
-        // Where some row does not see some key, 0 x NaN would be NaN: there, values that are not finite stay out of the product and
-        // are added key by key to the rows that give them a weight.
-        unsigned found = 0;
+        if (!masked || !holds_not_finite<DTYPE, C8, Rows::BYTES>(vt, lane)) {
 #pragma unroll
-        for (int fb = 0; fb < FB; ++fb) {
-            u32x4 w = __builtin_bit_cast(u32x4, Rows::template v_operand<DTYPE>(vt, 0, fb, lane));
-            if (masked) {
+            for (int fb = 0; fb < FB; ++fb) {
+                const s16x8 vf = Rows::template v_operand<DTYPE>(vt, 0, fb, lane);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const unsigned x = not_finite<DTYPE>(w[t]);
-                    found |= x;
-                    w[t] &= ~x;
-                }
+                for (int qb = 0; qb < QB; ++qb) O[fb][qb] = E::mfma16(vf, __builtin_bit_cast(s16x8, P[qb]), O[fb][qb]);
             }
+        } else {
+            // Where some row does not see some key, 0 x NaN would be NaN: there, values that are not finite stay out of the product and
+            // are added key by key to the rows that give them a weight.
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) O[fb][qb] = E::mfma16(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, P[qb]), O[fb][qb]);
-        }
-        if (__builtin_amdgcn_ballot_w64(found != 0) != 0) {
+            for (int fb = 0; fb < FB; ++fb) {
+                u32x4 w = __builtin_bit_cast(u32x4, Rows::template v_operand<DTYPE>(vt, 0, fb, lane));
+#pragma unroll
+                for (int t = 0; t < 4; ++t) w[t] &= ~not_finite<DTYPE>(w[t]);
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) O[fb][qb] = E::mfma16(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, P[qb]), O[fb][qb]);
+            }
             for (int j = 0; j < 32; ++j) {
                 float p[QB];
 #pragma unroll

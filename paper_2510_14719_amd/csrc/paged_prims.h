@@ -43,7 +43,7 @@ __device__ __forceinline__ int seq_of_token(const int* q_start, int sequences, i
 // units, those of long sequences are cut into pieces; which length to cut for is found on the device, from the lengths that are there, by every wave of the
 // kernel for itself: of 15 lengths, the longest sequence's x 2^(-c/4), the shortest that still makes no more pieces than there are compute units, if that
 // is worth the joining.  (On MI355X a tile of 64 keys takes 1.6 us, leaving partial results 6, joining them 8.  us cut / not: 12 sequences of 1 ... 777 new tokens,
-// 900 ... 4001 keys, 16 heads on 4, d 128 69 / 126; 8 of 64 new tokens, 4000 keys, the same heads 49 / 110.)
+// 900 ... 4001 keys, 16 heads on 4, d 128 67 / 97; 8 of 64 new tokens, 4000 keys, the same heads 40 / 96; one of 1024, 1024 keys 28 / 34.)
 constexpr int CHUNK_PARTS = 256;                // most pieces: a round of the compute units
 constexpr int CHUNK_UNCUT = 512;                // sequences up to this length are not cut
 constexpr float CHUNK_SAVES = 9.f, CHUNK_LEAST = 4.f;            // tiles that cutting has to save, and leaves in a piece at least
@@ -232,6 +232,28 @@ template <int D, int ES, int ROWS> struct CachedRows {
     }
 };
 
+// Whether any of the values of a tile in the LDS is not finite (16-bit ones, or E4M3 where C8).
+template <int DTYPE, bool C8, int BYTES> __device__ __forceinline__ bool holds_not_finite(const char* tile, int lane)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    unsigned worst[4] = {};
+#pragma unroll
+    for (int i = 0; i < BYTES / 1024; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(tile + i * 1024 + lane * 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (C8) worst[k] |= (w[k] & 0x7f7f7f7fu) + 0x01010101u;      // (only S.1111.111 carries into the sign)
+            else worst[k] = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, worst[k]), __builtin_bit_cast(u16x2, w[k] & 0x7fff7fffu)));
+        }
+    }
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        constexpr unsigned E = DTYPE == 0 ? 0x7c00u : 0x7f80u;
+        found |= C8 ? (worst[k] & 0x80808080u) != 0 : (worst[k] & 0xffffu) >= E || worst[k] >> 16 >= E;
+    }
+    return __builtin_amdgcn_ballot_w64(found) != 0;
+}
 // Non-finite values of a V^T operand: which halves of w have all exponent bits set, as a mask of the whole halves.
 template <int DTYPE> __device__ __forceinline__ unsigned not_finite(unsigned w)
 {

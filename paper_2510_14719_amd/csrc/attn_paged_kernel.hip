@@ -23,10 +23,11 @@ constexpr int NW = 4;                           // waves of a workgroup
 
 template <int D, int ES, int QB> struct FewLayout {
     typedef CachedRows<D, ES, 32> Rows;
-    static constexpr int STAGE = 2 * Rows::BYTES, SLOTS = 2, RING = NW * SLOTS * STAGE;
+    static constexpr int STAGE = 2 * Rows::BYTES, SLOTS = 2;
     static constexpr int JOIN = NW * (D / 16) * QB * 1024;   // O of every wave
-    static constexpr int SUMS = NW * QB * 16 * 8;            // reference and sum
-    static constexpr int SMEM = (RING > JOIN ? RING : JOIN) + SUMS;
+    static constexpr int SUMS = 1024;                        // first: reference and sum of every wave's rows
+    static_assert(NW * QB * 16 * 8 <= SUMS);
+    static constexpr int smem(int stages) { return SUMS + (stages * STAGE > JOIN ? stages * STAGE : JOIN); }
 };
 
 template <int DTYPE, bool C8, int D, int QB>
@@ -106,11 +107,11 @@ void attn_paged_few(PagedArgs a)
             k_off[hf][sub] = (unsigned)(r * a.token_bytes) + ((col ^ Rows::sw_k(hf * 16 + r)) * 16);
             v_off[hf][sub] = (unsigned)(r * a.token_bytes) + ((col ^ Rows::sw_v(hf * 16 + r)) * 16);
         }
-    const unsigned ring = (unsigned)(size_t)(LDS_AS void*)smem + wave * (Layout::SLOTS * Layout::STAGE);
+    const char* const ring = smem + Layout::SUMS + wave * Layout::STAGE;        // slot-major: a short piece uses the first stages only
     const char* const kh = uniform_ptr(a.k + h * a.head_bytes);
     const char* const vh = uniform_ptr(a.v + h * a.head_bytes);
     auto issue = [&](int step) __attribute__((always_inline)) -> unsigned {      // the halves of the step that lie in no page
-        const unsigned dst = ring + (step & 1) * Layout::STAGE;
+        const unsigned dst = (unsigned)(size_t)(LDS_AS const void*)(ring + (step & 1) * (NW * Layout::STAGE));
         const int key = k0 + (step * NW + wave) * 32;
         unsigned bad = 0;
 #pragma unroll
@@ -160,7 +161,7 @@ void attn_paged_few(PagedArgs a)
 
     for (int step = 0; step < steps; ++step) {
         if (step + 1 < steps) wait_vmcnt<PIECES>(); else wait_vmcnt<0>();
-        const char* const kt = smem + wave * (Layout::SLOTS * Layout::STAGE) + (step & 1) * Layout::STAGE;
+        const char* const kt = ring + (step & 1) * (NW * Layout::STAGE);
         const char* const vt = kt + Rows::BYTES;
         const int key = k0 + (step * NW + wave) * 32;
         f32x4 S[2][QB];
@@ -255,13 +256,14 @@ void attn_paged_few(PagedArgs a)
     }
 
     // ---- join the waves: each takes its share of the features
-    float* const sums = reinterpret_cast<float*>(smem + Layout::SMEM - Layout::SUMS);
+    float* const sums = reinterpret_cast<float*>(smem);
+    char* const join = smem + Layout::SUMS;
     __syncthreads();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         L[qb] = groups_sum(L[qb]);
 #pragma unroll
-        for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(smem + ((wave * FB + fb) * QB + qb) * 1024 + lane * 16) = O[fb][qb];
+        for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(join + ((wave * FB + fb) * QB + qb) * 1024 + lane * 16) = O[fb][qb];
         if (lg == 0) *reinterpret_cast<f32x2*>(sums + ((wave * QB + qb) * 16 + lc) * 2) = f32x2{m_run[qb], L[qb]};
     }
     __syncthreads();
@@ -288,7 +290,7 @@ void attn_paged_few(PagedArgs a)
             const int fb = wave * (FB / NW) + f;
             f32x4 x = f32x4(0.f);
 #pragma unroll
-            for (int v = 0; v < NW; ++v) x += *reinterpret_cast<const f32x4*>(smem + ((v * FB + fb) * QB + qb) * 1024 + lane * 16) * w[v];
+            for (int v = 0; v < NW; ++v) x += *reinterpret_cast<const f32x4*>(join + ((v * FB + fb) * QB + qb) * 1024 + lane * 16) * w[v];
             if (!real) continue;
             if (whole) {
                 const u32x2 y = {E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};
@@ -395,11 +397,15 @@ int launch_few(const PagedArgs& a, hipStream_t stream)
     typedef FewLayout<D, C8 ? 1 : 2, QB> Layout;
     auto kern = attn_paged_few<DTYPE, C8, D, QB>;
     static PerDeviceOnce once;
-    if (once.prepare(reinterpret_cast<const void*>(kern), Layout::SMEM) < 0) return -1;
+    constexpr int STAGES = NW * Layout::SLOTS;
+    if (once.prepare(reinterpret_cast<const void*>(kern), Layout::smem(STAGES)) < 0) return -1;
     PagedArgs arg = a;
     void* args[] = {&arg};
+    // Where all keys fit fewer stages, the others are not asked for and more workgroups fit a compute unit.  (us so / with all stages, d 128:
+    // 156 sequences of 7 keys, 16 heads 22 / 39; 256 of 100, 32 heads on 8 31 / 48.)
+    const int blocks = a.max_kv < STAGES * 32 ? (a.max_kv + 31) / 32 : STAGES, smem = Layout::smem(blocks);
     const long long grid = (long long)a.sequences * a.splits * (a.heads / a.group);
-    return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, Layout::SMEM, stream) == hipSuccess ? 0 : -1;
+    return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, smem, stream) == hipSuccess ? 0 : -1;
 }
 
 template <int DTYPE, bool C8, int D>

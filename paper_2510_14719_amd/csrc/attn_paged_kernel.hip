@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "launch_once.h"
 #include "paged_launch.h"
 #include "paged_prims.h"
@@ -366,25 +368,39 @@ void attn_paged_join_chunks(PagedArgs a)
     const int key_heads = a.heads / a.group, h = blockIdx.x % key_heads, e = threadIdx.x % LANES;
     if ((int)blockIdx.x >= a.chunk_what[a.chunk_parts * 4]) return;
     const u32x4 what = *reinterpret_cast<const u32x4*>(a.chunk_what + blockIdx.x * 4);
-    const int s = (int)what[0], n = (int)what[2];            // (a chunk is cut into 14 pieces at most)
+    const int s = (int)what[0], n = (int)what[2];
     if (n < 2) return;
     const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
     const long long step = (long long)key_heads * PAGED_CHUNK_ROWS;      // from a piece to the next
     const int r = blockIdx.y * (256 / LANES) + threadIdx.x / LANES, row = (int)what[1] * PAGED_CHUNK_ROWS + r, tok = row / a.group, head = h * a.group + row % a.group;
     if (tok >= seq.n) return;
     const long long first = (long long)what[3] * PAGED_CHUNK_ROWS + r;
-    const int k = min(threadIdx.x & 15, n - 1);
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.chunk_ml + (first + k * step) * 2);       // a piece a lane
+    const int lane = threadIdx.x & 15;          // 16 lanes have 16 pieces' references and sums
+    f32x2 ml = *reinterpret_cast<const f32x2*>(a.chunk_ml + (first + min(lane, n - 1) * step) * 2);
     float m = ml[0];
+    for (int k = 16 + lane; k < n; k += 16) m = __builtin_fmaxf(m, a.chunk_ml[(first + k * step) * 2]);
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d));
-    const float w = __builtin_amdgcn_exp2f(ml[0] - m);
-    float l = (int)(threadIdx.x & 15) < n ? ml[1] * w : 0.f;
+    float l = 0.f;
+    f32x4 x = f32x4(0.f);
+    for (int k = 0; k < n; k += 16) {
+        if (k > 0) ml = *reinterpret_cast<const f32x2*>(a.chunk_ml + (first + min(k + lane, n - 1) * step) * 2);
+        const float w = __builtin_amdgcn_exp2f(ml[0] - m);
+        l += k + lane < n ? ml[1] * w : 0.f;
+        const int some = min(16, n - k);
+        auto add = [&](auto count, int j) __attribute__((always_inline)) {       // so many loads under way
+#pragma unroll
+            for (int i = j; i < j + decltype(count)::value; ++i) {
+                const f32x4 part = *reinterpret_cast<const f32x4*>(a.chunk_o + (first + min(k + i, n - 1) * step) * D + e * 4) * __shfl(w, (threadIdx.x & 48) + i);
+                x += i < some ? part : f32x4(0.f);
+            }
+        };
+        int j = 0;
+        for (; j + 2 < some; j += 8) add(std::integral_constant<int, 8>(), j);
+        if (j < some) add(std::integral_constant<int, 2>(), j);
+    }
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
-    f32x4 x = f32x4(0.f);
-#pragma unroll 7
-    for (int j = 0; j < n; ++j) x += *reinterpret_cast<const f32x4*>(a.chunk_o + (first + j * step) * D + e * 4) * __shfl(w, (threadIdx.x & 48) + j);
     const int t = seq.q0 + tok;
     const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
     *reinterpret_cast<u32x2*>(a.o + t * a.o_token + head * a.o_head + e * 8) = u32x2{E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};

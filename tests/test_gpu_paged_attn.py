@@ -69,6 +69,20 @@ def test_a_long_chunk(kv, dtype, cache):
     run(kv, Batch([(513, 513), (2, 600)], 2, 1, 64, dtype, cache, 64), what="chunk of 513")
 
 
+@pytest.mark.parametrize("d,dtype,cache", [(128, "bf16", "bf16"), (64, "fp16", "e4m3")])
+@pytest.mark.parametrize("lens", [[(12, 17003)], [(12, 17003), (9, 5003), (40, 1200)]])
+def test_chunks_cut_into_many_pieces(kv, d, dtype, cache, lens):
+    run(kv, Batch(lens, 4, 1, d, dtype, cache, 64, peaky=True))
+
+
+@pytest.mark.parametrize("d,dtype,cache", [(128, "bf16", "bf16"), (64, "fp16", "fp16"), (128, "fp16", "e4m3")])
+@pytest.mark.parametrize("longest", [1, 32, 33, 64, 129, 224, 225, 256, 257])
+def test_the_shortest_sequences(kv, d, dtype, cache, longest):
+    lens = [(1, longest), (1, 1), (min(3, longest), longest), (1, (longest + 1) // 2)]
+    run(kv, Batch(lens, 4, 2, d, dtype, cache, 16))
+    run(kv, Batch([(min(n * 5, k), k) for n, k in lens], 4, 1, d, dtype, cache, 16))
+
+
 @pytest.mark.parametrize("G,Hk,dtype,cache", [(4, 1, "bf16", "bf16"), (2, 2, "fp16", "e4m3")])
 def test_many_sequences_of_all_kinds(kv, G, Hk, dtype, cache):
     """More than a wave has lanes: single tokens, none at all, and chunks that are cut along their keys between them."""

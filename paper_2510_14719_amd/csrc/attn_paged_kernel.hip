@@ -49,10 +49,12 @@ void attn_paged_few(PagedArgs a)
     int id = blockIdx.x;
     const int h = id % key_heads;
     id /= key_heads;
-    const int sp = id % a.splits, s = id / a.splits;
+    const int sp = id % a.splits;
+    id /= a.splits;
+    const int tile = a.row_tiles - 1 - id % a.row_tiles, s = id / a.row_tiles;
     const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-    if (seq.n == 0 || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(0, ROWS, seq.n, a.group, seq.kv, a.causal), per = paged_piece_keys(keys, a.split);
+    if (tile * ROWS >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
+    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal), per = paged_piece_keys(keys, a.split);
     const int k0 = sp * per, k1 = min(keys, k0 + per);
     if (sp > 0 && k0 >= keys) return;
     const bool whole = keys <= per;
@@ -71,7 +73,7 @@ void attn_paged_few(PagedArgs a)
     long long o_row[QB];                        // token * heads + head, -1 behind the last row
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int r = qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group;
+        const int r = tile * ROWS + qb * 16 + lc, tok = r / a.group, head = h * a.group + r % a.group;
         const bool real = tok < seq.n;
         const int t = seq.q0 + (real ? tok : seq.n - 1);
         const char* const at = a.q + t * a.q_token + head * a.q_head + lg * 16;
@@ -80,7 +82,7 @@ void attn_paged_few(PagedArgs a)
         last_key[qb] = a.causal ? min(seq.kv - seq.n + tok, keys - 1) : keys - 1;
         o_row[qb] = real ? (long long)t * a.heads + head : -1;
     }
-    const int first_last = a.causal ? seq.kv - seq.n : keys - 1;   // what the first row sees
+    const int first_last = a.causal ? seq.kv - seq.n + tile * ROWS / a.group : keys - 1;   // what the first row sees
 
     const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
     // The reference before the first score: the most negative float whose scaled value is finite.  (-inf would make NaN of rows whose
@@ -320,10 +322,10 @@ void attn_paged_join(PagedArgs a)
     __shared__ float s_l[GROUPS];
     const int lane = threadIdx.x & 63, group = threadIdx.x / LANES, e = threadIdx.x % LANES;
     // the r-th row of key head h of sequence s
-    const int key_heads = a.heads / a.group, most = min(a.rows, a.max_q * a.group), r = blockIdx.x % most, h = blockIdx.x / most % key_heads;
+    const int key_heads = a.heads / a.group, most = min(a.row_tiles * a.rows, a.max_q * a.group), r = blockIdx.x % most, h = blockIdx.x / most % key_heads;
     const SeqRange seq = seq_range(a.q_start, a.kv_len, blockIdx.x / most / key_heads, a.tokens, a.max_q, a.max_kv);
     if (r >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(0, a.rows, seq.n, a.group, seq.kv, a.causal);
+    const int keys = paged_tile_keys(r / a.rows, a.rows, seq.n, a.group, seq.kv, a.causal);
     const int per = paged_piece_keys(keys, a.split);
     if (keys <= per) return;
     const int n = (keys + per - 1) / per, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
@@ -420,7 +422,7 @@ int launch_few(const PagedArgs& a, hipStream_t stream)
     // Where all keys fit fewer stages, the others are not asked for and more workgroups fit a compute unit.  (us so / with all stages, d 128:
     // 156 sequences of 7 keys, 16 heads 22 / 39; 256 of 100, 32 heads on 8 31 / 48.)
     const int blocks = a.max_kv < STAGES * 32 ? (a.max_kv + 31) / 32 : STAGES, smem = Layout::smem(blocks);
-    const long long grid = (long long)a.sequences * a.splits * (a.heads / a.group);
+    const long long grid = (long long)a.sequences * a.row_tiles * a.splits * (a.heads / a.group);
     return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, smem, stream) == hipSuccess ? 0 : -1;
 }
 
@@ -436,7 +438,7 @@ int launch_all(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
         rc = hipLaunchKernel(reinterpret_cast<const void*>(attn_paged_join_chunks<DTYPE, C8, D>), dim3((unsigned)(plan.chunk_tiles < a.chunk_parts ? plan.chunk_tiles : a.chunk_parts), PAGED_CHUNK_ROWS / (1024 / D)), dim3(256), args, 0, stream) == hipSuccess ? 0 : -1;
     if (rc != 0 || a.splits == 1) return rc;
     // (few rows: 4 waves a row, to have many parts under way; many: one)
-    const int most = a.max_q * a.group < a.rows ? a.max_q * a.group : a.rows;
+    const int most = a.max_q * a.group < a.row_tiles * a.rows ? a.max_q * a.group : a.row_tiles * a.rows;
     const long long grid = (long long)a.sequences * (a.heads / a.group) * most;
     const void* const kern = grid <= 1024 ? reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D, 4>) : reinterpret_cast<const void*>(attn_paged_join<DTYPE, C8, D, 1>);
     return hipLaunchKernel(kern, dim3((unsigned)grid), dim3(grid <= 1024 ? 256 : 64), args, 0, stream) == hipSuccess ? 0 : -1;
@@ -452,24 +454,39 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
     PagedPlan p{};
     p.splits = 1;
     p.split = whole;
-    // Sequences of up to 32 rows take small tiles, longer ones chunks.  One sequence takes one kind.
-    p.rows = most <= 16 ? 16 : 32;
-    p.few_rows = most <= 32 || (long long)sequences * key_heads > 64 ? 32 : 0;
+    // Small tiles of 16 or 32 rows, or chunks of 256.  The former have many workgroups, fit for short calls, the latter feed the matrix cores better.  In keys that the places
+    // of the chip walk through one after the other: chunks of sequences that they are cut for (or are not) cost as much as 400 (900) keys more.  us chunks / small tiles, d 128, 16-bit,
+    // 16 heads, one prompt of 64 8.3 / 5.7, 256 15.5 / 6.9, 512 20.8 / 12.1, 1024 29.5 / 25.2; 32 heads on 8, 64 tokens of 1000 21.0 / 12.8, 256 of 4000 35.2 / 51.8,
+    // one prompt of 1024 37.5 / 47.3.  Over 432 calls of all four kinds 23 % less on the mean than chunks for all with more than 32 rows, at most 9 % more.
+    const long long key_bytes = 2ll * d * cache_bytes;
+    auto workgroups = [&](int rows) { return (double)((most + rows - 1) / rows) * sequences * key_heads; };
+    auto places = [&](int rows, int kv) {       // what the LDS and the registers hold on 256 compute units
+        const int stages = kv < 256 ? (kv + 31) / 32 : 8;
+        const long long ring = stages * 32 * key_bytes, join = rows * d * 16, fit = (160 << 10) / (1024 + (ring > join ? ring : join)), regs = rows == 32 ? (d == 128 ? 1 : 2) : d == 128 ? 2 : cache_bytes == 2 ? 3 : 4;
+        return 256 * (fit < regs ? fit : regs);
+    };
+    const double small = workgroups(32), chip = places(16, 256);
+    const double keys = max_q < max_kv ? max_kv - 0.5 * max_q : 0.5 * max_kv;        // of a row on the mean, as most calls are
+    const bool all_small = most <= 32 || (small <= 256 + chip && small * keys / chip <= (max_kv > 1024 ? 400 : 900) + workgroups(256) * keys / 256);
+    p.few_rows = all_small ? 1 << 30 : (long long)sequences * key_heads > 64 ? 32 : 0;
+    // 16 rows where they have a place each (with the pieces of long sequences) or, with more rows, no more rounds than those of 32: a step of 128 keys takes 1.0 us with 16 rows, 1.5 with 32.
+    const double parts = max_kv > 1024 ? max_kv / 512. : 1., rounds = parts * workgroups(16) / places(16, max_kv), rounds32 = parts * small / places(32, max_kv);
+    p.rows = most <= 16 || (all_small && (rounds <= 1. || (most > 32 && rounds <= rounds32))) ? 16 : 32;
+    p.row_tiles = all_small ? (int)((most + p.rows - 1) / p.rows) : 1;
     if (p.few_rows) {
         // Pieces: about one for every workgroup that the chip holds (one a compute unit with rows of 256 bytes, two with 128, four with 64), of 512 keys at least;
         // where there are 512 workgroups or more anyway, pieces only serve to even out lengths, and have 1.25 MiB of keys and values.  A piece
         // costs 4 us besides its keys, the joining 6.  us at most keys of a piece 512 / 768 / 1536 / 2560 / 4096, d 128, 32 heads on 8:
         // 64 sequences of 4000 218 / 211 / 197 / 191 / 183; of 300 ... 16384 260 / 232 / 211 / 211 / 251; one of 32768 35 / 38 / 31 / 37 / 49;
         // one of 2000 13 / 15 / 17 / 22 (whole); 8 of 900, whole 15.
-        const long long units = (long long)sequences * key_heads, key_bytes = 2ll * d * cache_bytes;
-        const long long even = (5 << 18) / key_bytes, chip = 256 * (512 / key_bytes);
-        long long split = units >= 512 ? even : units * max_kv / chip;
+        const long long units = (long long)sequences * key_heads * p.row_tiles, even = (5 << 18) / key_bytes;
+        long long split = units >= 512 ? even : units * max_kv / (256 * (512 / key_bytes));
         if (split < 512) split = 512;
         if (max_kv <= (units >= 512 ? even * 8 / 5 : 1024)) split = whole;
         if (split < whole) p.split = (int)((split + 127) / 128 * 128);
         p.splits = (int)((max_kv + p.split - 1) / p.split);
     }
-    if (most > 32) {
+    if (!all_small) {
         const long long each = (most + PAGED_CHUNK_ROWS - 1) / PAGED_CHUNK_ROWS * sequences, all = (long long)tokens * group / PAGED_CHUNK_ROWS + sequences;
         p.chunk_tiles = (each < all ? each : all) * key_heads;
         if (max_kv > CHUNK_UNCUT) p.chunk_parts = CHUNK_PARTS;

@@ -140,7 +140,7 @@ bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads
 {
     const i64 most = 1ll << 23;                 // workgroups of 512 threads: a grid has less than 2^32
     auto fits = [&](i64 tiles, i64 splits) { return tiles < most && tiles * splits < most && tiles * splits * c->heads < most; };
-    return fits(p.splits, b->sequences) && fits(p.chunk_tiles, 1) && fits(b->sequences, p.rows);
+    return fits((i64)p.splits * p.row_tiles, b->sequences) && fits(p.chunk_tiles, 1) && fits((i64)b->sequences * p.row_tiles, p.rows);
 }
 
 int check_book(const kv_book* b)
@@ -255,6 +255,7 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.causal = causal != 0;
     a.few_rows = p.few_rows;
     a.rows = p.rows;
+    a.row_tiles = p.row_tiles;
     a.split = p.split;
     a.splits = p.splits;
     a.chunk_parts = p.chunk_parts;

@@ -49,12 +49,25 @@ void attn_paged_few(PagedArgs a)
     int id = blockIdx.x;
     const int h = id % key_heads;
     id /= key_heads;
-    const int sp = id % a.splits;
-    id /= a.splits;
-    const int tile = a.row_tiles - 1 - id % a.row_tiles, s = id / a.row_tiles;
-    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    FewPiece mine;
+    if (a.few_room > 0) {
+        const SeqRange first = few_seq(a, lane);
+        const float inverse = few_cut(a, first, lane);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.few_inverse = inverse;
+        mine = few_numbered(a, first, inverse, id, lane);
+        if (mine.s < 0) return;
+    } else {
+        mine.piece = id % a.splits;
+        id /= a.splits;
+        mine.tile = a.row_tiles - 1 - id % a.row_tiles;
+        mine.s = id / a.row_tiles;
+        mine.pieces = 0;
+        mine.seq = seq_range(a.q_start, a.kv_len, mine.s, a.tokens, a.max_q, a.max_kv);
+    }
+    const int s = __builtin_amdgcn_readfirstlane(mine.s), tile = __builtin_amdgcn_readfirstlane(mine.tile), sp = __builtin_amdgcn_readfirstlane(mine.piece);
+    const SeqRange seq = {__builtin_amdgcn_readfirstlane(mine.seq.q0), __builtin_amdgcn_readfirstlane(mine.seq.n), __builtin_amdgcn_readfirstlane(mine.seq.kv)};
     if (tile * ROWS >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal), per = paged_piece_keys(keys, a.split);
+    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal), per = a.few_room > 0 ? few_piece_keys(mine.pieces, keys) : paged_piece_keys(keys, a.split);
     const int k0 = sp * per, k1 = min(keys, k0 + per);
     if (sp > 0 && k0 >= keys) return;
     const bool whole = keys <= per;
@@ -326,7 +339,7 @@ void attn_paged_join(PagedArgs a)
     const SeqRange seq = seq_range(a.q_start, a.kv_len, blockIdx.x / most / key_heads, a.tokens, a.max_q, a.max_kv);
     if (r >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
     const int keys = paged_tile_keys(r / a.rows, a.rows, seq.n, a.group, seq.kv, a.causal);
-    const int per = paged_piece_keys(keys, a.split);
+    const int per = a.few_room > 0 ? few_piece_keys(few_pieces(*a.few_inverse, seq.kv), keys) : paged_piece_keys(keys, a.split);
     if (keys <= per) return;
     const int n = (keys + per - 1) / per, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
     const long long row = (long long)t * a.heads + head, all = (long long)a.tokens * a.heads;
@@ -422,7 +435,7 @@ int launch_few(const PagedArgs& a, hipStream_t stream)
     // Where all keys fit fewer stages, the others are not asked for and more workgroups fit a compute unit.  (us so / with all stages, d 128:
     // 156 sequences of 7 keys, 16 heads 22 / 39; 256 of 100, 32 heads on 8 31 / 48.)
     const int blocks = a.max_kv < STAGES * 32 ? (a.max_kv + 31) / 32 : STAGES, smem = Layout::smem(blocks);
-    const long long grid = (long long)a.sequences * a.row_tiles * a.splits * (a.heads / a.group);
+    const long long grid = (a.few_room > 0 ? a.few_room : (long long)a.sequences * a.row_tiles * a.splits) * (a.heads / a.group);
     return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, smem, stream) == hipSuccess ? 0 : -1;
 }
 
@@ -474,16 +487,36 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
     p.rows = most <= 16 || (all_small && (rounds <= 1. || (most > 32 && rounds <= rounds32))) ? 16 : 32;
     p.row_tiles = all_small ? (int)((most + p.rows - 1) / p.rows) : 1;
     if (p.few_rows) {
-        // Pieces: about one for every workgroup that the chip holds (one a compute unit with rows of 256 bytes, two with 128, four with 64), of 512 keys at least;
-        // where there are 512 workgroups or more anyway, pieces only serve to even out lengths, and have 1.25 MiB of keys and values.  A piece
-        // costs 4 us besides its keys, the joining 6.  us at most keys of a piece 512 / 768 / 1536 / 2560 / 4096, d 128, 32 heads on 8:
-        // 64 sequences of 4000 218 / 211 / 197 / 191 / 183; of 300 ... 16384 260 / 232 / 211 / 211 / 251; one of 32768 35 / 38 / 31 / 37 / 49;
-        // one of 2000 13 / 15 / 17 / 22 (whole); 8 of 900, whole 15.
-        const long long units = (long long)sequences * key_heads * p.row_tiles, even = (5 << 18) / key_bytes;
-        long long split = units >= 512 ? even : units * max_kv / (256 * (512 / key_bytes));
-        if (split < 512) split = 512;
-        if (max_kv <= (units >= 512 ? even * 8 / 5 : 1024)) split = whole;
-        if (split < whole) p.split = (int)((split + 127) / 128 * 128);
+        // Pieces, of 512 keys at least: where the workgroups are fewer than the places, as many as these are, found on the device; where there are 512 workgroups or more
+        // anyway, pieces only serve to even out lengths, and have 1.25 MiB of keys and values.  A piece costs 4 us besides its keys, the joining
+        // 6.  (us at most keys of a piece 512 / 768 / 1536 / 2560 / 4096, d 128, 32 heads on 8: 64 sequences of 4000 218 / 211 / 197 / 191 / 183; of
+        // 300 ... 16384 260 / 232 / 211 / 211 / 251.)
+        const long long tiles = (long long)sequences * p.row_tiles, units = tiles * key_heads, even = (5 << 18) / key_bytes;
+        if (units >= 512) {
+            if (max_kv > even * 8 / 5) p.split = (int)((even + 127) / 128 * 128);
+        } else if (max_kv > 1024) {
+            // One piece a place, or two or three one after the other where that evens them out (sequences of 9000 of 4 tokens each over E4M3: 37, 32 heads on 4, d 128 115 / 95 us, 20, 128 heads on 16,
+            // d 64 106 / 90) and reading the cache takes less time anyway.
+            const double alone = max_kv / 128. * (p.rows == 16 ? 1. : 1.5), reading = (double)units * max_kv * key_bytes / 5.5e6;
+            long long room = 0;
+            double best = 1e30;
+            for (int rounds = 1; rounds <= 3; ++rounds) {
+                const long long all = places(p.rows, 256) * rounds, k = all / units;
+                const double time = k == 0 ? 1e30 : rounds * (alone / k + 4.);
+                if (time < 0.9 * best && best > reading) {
+                    best = time;
+                    room = all / key_heads;
+                }
+            }
+            if (room > tiles) {                 // (else whole)  The longest sequence may have all pieces that the others leave, or all are alike.
+                const long long least = max_kv / (room - tiles + 1), alike = (max_kv + room / tiles - 1) / (room / tiles);
+                p.split = (int)(least > 512 ? least : 512);
+                p.split_max = (int)(alike > p.split ? alike : p.split);
+                if (sequences == 1 || sequences > 128) p.split = p.split_max;          // (many: finding out would take longer than it saves)
+                if (p.split < p.split_max) p.few_room = (int)room;
+                else if (p.split < whole) p.split = (p.split + 63) / 64 * 64;
+            }
+        }
         p.splits = (int)((max_kv + p.split - 1) / p.split);
     }
     if (!all_small) {

@@ -134,7 +134,7 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? (i64)p.splits * b->tokens * heads : 0; }
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
-    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0);
+    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.few_room ? 16 : 0);
 }
 bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
@@ -243,6 +243,7 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.part_ml = a.chunk_o + chunk * cache->d;
     a.chunk_ml = a.part_ml + few * 2;
     a.chunk_what = (int*)(a.chunk_ml + chunk * 2);
+    a.few_inverse = (float*)(a.chunk_what + (p.chunk_parts ? (p.chunk_parts + 1) * 4 : 0));
     a.sequences = batch->sequences;
     a.tokens = batch->tokens;
     a.table_stride = batch->table_stride;
@@ -256,6 +257,10 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.few_rows = p.few_rows;
     a.rows = p.rows;
     a.row_tiles = p.row_tiles;
+    a.few_room = p.few_room;
+    a.few_finest = 1.f / (float)p.split;
+    a.few_coarsest = p.few_room ? 1.f / (float)p.split_max : 0.f;
+    a.few_step = p.few_room ? std::log2((float)p.split_max / (float)p.split) / 63.f : 0.f;
     a.split = p.split;
     a.splits = p.splits;
     a.chunk_parts = p.chunk_parts;

@@ -26,6 +26,9 @@ struct PagedArgs {
     int few_rows;                                            // sequences with more rows (new tokens x group) than this go by chunks of PAGED_CHUNK_ROWS
     int rows, row_tiles, split, splits;                      // the others: rows per workgroup, row tiles of the longest one, most keys of a piece (a multiple of 128), pieces of
                                                              // the longest
+    int few_room;                                            // > 0: how long their pieces are is found on the device (few_cut), so that there are at most so many (of every key head)
+    float few_finest, few_step, few_coarsest;                // 1 / keys: of the shortest, log2 of a step, of the longest
+    float* few_inverse;                                      // what was found, for the join
     int chunk_parts;                                         // room for partial results of chunks, in workgroups (0: chunks are not cut along the keys)
     float *chunk_o, *chunk_ml;                               // [workgroup][PAGED_CHUNK_ROWS][d], [..][2]
     int* chunk_what;                                         // [chunk of a key head][4]: sequence, chunk in it, pieces, workgroup of the first; behind the last [..][0] their number
@@ -36,7 +39,7 @@ constexpr int PAGED_CHUNK_ROWS = 256;                        // query rows (toke
 
 // How a call is laid out (chosen by its sizes alone, so that the workspace is known beforehand).
 struct PagedPlan {
-    int few_rows, rows, row_tiles, split, splits, chunk_parts;           // as in PagedArgs (few_rows 0: all sequences go by chunks)
+    int few_rows, rows, row_tiles, split, splits, few_room, split_max, chunk_parts;      // as in PagedArgs (few_rows 0: all sequences go by chunks)
     long long chunk_tiles;                                   // chunks of all sequences, at most; 0: none does
 };
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes);

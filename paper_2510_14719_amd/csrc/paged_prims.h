@@ -37,6 +37,68 @@ __device__ __forceinline__ int seq_of_token(const int* q_start, int sequences, i
     return -1;
 }
 
+// ---- how the sequences of small tiles are cut along their keys
+//
+// Where their workgroups are fewer than the chip has places (few_room > 0), every wave finds for itself the shortest of some lengths whose pieces, of all
+// sequences together, still have a place each, and which piece its workgroup has.  (One token each, 32 heads on 8,
+// d 128, with pieces of one length that the host chose from the longest sequence / so: 11 of 9000 102 / 76 us, 3 of 9000 34.8 / 27.3, 9 of 2000 ... 9000 54 / 40.)
+// Pieces of a sequence, cut for 1 / inverse keys (a row tile of it has as many, of its own keys).
+__device__ __forceinline__ int few_pieces(float inverse, int kv) { return max(1, (int)__builtin_ceilf(__builtin_fmaf((float)kv, inverse, -0.001f))); }
+__device__ __forceinline__ int few_tiles(const PagedArgs& a, const SeqRange& seq)
+{
+    const int rows = seq.n * a.group;
+    return rows > a.few_rows ? 0 : (rows + a.rows - 1) / a.rows;
+}
+__device__ __forceinline__ SeqRange few_seq(const PagedArgs& a, int s)
+{
+    return s < a.sequences ? seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv) : SeqRange{0, 0, 0};
+}
+// (`first`: the first 64 sequences, a lane each; a lane has a length)
+__device__ inline float few_cut(const PagedArgs& a, const SeqRange& first, int lane)
+{
+    const float inverse = lane == 63 ? a.few_coarsest : a.few_finest * __builtin_amdgcn_exp2f(-a.few_step * lane);
+    int pieces = 0;
+    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+        const SeqRange seq = s0 == 0 ? first : few_seq(a, s0 + lane);
+        const int tiles = few_tiles(a, seq);
+        unsigned long long there = __builtin_amdgcn_ballot_w64(tiles > 0);
+        while (there) {
+            const int i = __builtin_ctzll(there);
+            there &= there - 1;
+            pieces += __builtin_amdgcn_readlane(tiles, i) * few_pieces(inverse, __builtin_amdgcn_readlane(seq.kv, i));
+        }
+    }
+    const unsigned long long fits = __builtin_amdgcn_ballot_w64(lane == 63 || pieces <= a.few_room);     // (the longest: the host has seen to it)
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), __builtin_ctzll(fits)));
+}
+// The piece with a number; s = -1 behind the last.
+struct FewPiece {
+    int s, tile, piece, pieces;
+    SeqRange seq;
+};
+__device__ inline FewPiece few_numbered(const PagedArgs& a, const SeqRange& first, float inverse, int left, int lane)
+{
+    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+        const SeqRange seq = s0 == 0 ? first : few_seq(a, s0 + lane);
+        const int pieces = few_pieces(inverse, seq.kv), own = few_tiles(a, seq) * pieces;
+        int sum = own;                          // with those of the lanes before
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(sum, d);
+            if (lane >= d) sum += x;
+        }
+        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(sum > left);
+        if (beyond) {
+            const int at = __builtin_ctzll(beyond), n = __builtin_amdgcn_readlane(pieces, at), inside = left - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(own, at));
+            return {s0 + at, inside / n, inside % n, n, {__builtin_amdgcn_readlane(seq.q0, at), __builtin_amdgcn_readlane(seq.n, at), __builtin_amdgcn_readlane(seq.kv, at)}};
+        }
+        left -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return {-1, 0, 0, 1, {0, 0, 0}};
+}
+// Keys of a piece of a row tile with so many keys.
+__device__ __forceinline__ int few_piece_keys(int pieces, int keys) { return max(((keys + pieces - 1) / pieces + 63) / 64 * 64, 64); }
+
 // ---- how chunks are cut along their keys
 //
 // Chunks of the sequences with more rows than few_rows are numbered through, the last one of a sequence first.  Where they are fewer than the chip has compute

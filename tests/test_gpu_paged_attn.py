@@ -92,6 +92,16 @@ def test_many_sequences_of_all_kinds(kv, G, Hk, dtype, cache):
     run(kv, Batch(lens, G * Hk, Hk, 64, dtype, cache, 16, pad=5))
 
 
+@pytest.mark.parametrize("d,dtype,cache", [(128, "fp16", "fp16"), (64, "bf16", "e4m3")])
+@pytest.mark.parametrize("count", [5, 63, 64, 65, 120, 140])
+def test_pieces_of_sequences_of_all_lengths(kv, count, d, dtype, cache):
+    lens = [((1, 3, 0, 2)[i % 4], 1 + 211 * i * i % 2900 if i % 3 else 7 + i) for i in range(count)]
+    lens = [(min(n, k), k) for n, k in lens]
+    b = Batch(lens, 6, 1, d, dtype, cache, 32, pad=3)
+    assert kv.attn_paged_workspace(b.q.cuda(), b.k_cache.cuda(), count, b.max_q, b.max_kv) > 0
+    run(kv, b)
+
+
 def test_two_calls_at_once(kv):
     """On two streams, each with a workspace of its own."""
     b = Batch([(1, 3000), (2, 2100), (40, 1300)], 4, 2, 128, "bf16", "bf16", 16)

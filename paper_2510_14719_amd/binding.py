@@ -121,7 +121,7 @@ def torch_build() -> str:
 class _NoExtension:
     """In the place of the extension where there is none: takes nothing."""
     attn_fwd = attn_fwd_fp8 = gemm_nt = gemm_nt_fp8 = staticmethod(lambda *args: NotImplemented)
-    attn_paged = kv_append = rope = kv_reserve = kv_free = kv_fork = staticmethod(lambda *args: NotImplemented)
+    attn_paged = kv_append = rope = kv_reserve = kv_free = kv_fork = kv_compact = kv_copy_pages = staticmethod(lambda *args: NotImplemented)
 
 
 def _load_fast():
@@ -141,7 +141,8 @@ def _load_fast():
             _fast = _NoExtension
             return _fast
         ext.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.attn_fwd, lib.attn_fwd_fp8, lib.gemm_nt, lib.gemm_nt_fp8)))
-        ext.bind_kv(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.attn_paged, lib.kv_append, lib.rope, lib.kv_reserve, lib.kv_free, lib.kv_fork)))
+        ext.bind_kv(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.attn_paged, lib.kv_append, lib.rope, lib.kv_reserve, lib.kv_free, lib.kv_fork,
+                                                                                    lib.kv_compact, lib.kv_copy_pages)))
         os.register_at_fork(after_in_child=ext.disable)
         _fast = ext
     return _fast

@@ -175,6 +175,8 @@ struct KvCalls {
     decltype(&::kv_reserve) kv_reserve;
     decltype(&::kv_free) kv_free;
     decltype(&::kv_fork) kv_fork;
+    decltype(&::kv_compact) kv_compact;
+    decltype(&::kv_copy_pages) kv_copy_pages;
 } kv_calls;
 bool kv_enabled = false;
 
@@ -458,24 +460,52 @@ PyObject* kv_fork_(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
-// bind_kv(attn_paged, kv_append, rope, kv_reserve, kv_free, kv_fork): addresses of the functions of the loaded library
+// (k_cache, v_cache, ref, table, kv_len, workspace, stream)
+PyObject* kv_compact_(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return kv_call<7>(args, n, [](Args& a) {
+        const kv_pages c = pages_of(a, 0, 1, -1, -1, true);
+        const kv_book b = book_of(a, 2, c.page_size);
+        int64_t bytes;
+        void* const workspace = a.array(5, at::kByte, -1, &bytes);
+        void* const stream = a.stream(6);
+        return unlocked([&] { return kv_calls.kv_compact(&c, &b, workspace, bytes, stream); });
+    });
+}
+
+// (k_cache, v_cache, src, dst, stream)
+PyObject* kv_copy_pages_(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return kv_call<5>(args, n, [](Args& a) {
+        const kv_pages c = pages_of(a, 0, 1, -1, -1, true);
+        int64_t count;
+        const int* const src = (const int*)a.array(2, at::kInt, -1, &count);
+        const int* const dst = (const int*)a.array(3, at::kInt, count);
+        want(a.tensor(2).dim() == 1 && a.tensor(3).dim() == 1 && count <= KV_MAX_LIST);
+        void* const stream = a.stream(4);
+        return unlocked([&] { return kv_calls.kv_copy_pages(&c, src, dst, (int)count, stream); });
+    });
+}
+
+// bind_kv(attn_paged, kv_append, rope, kv_reserve, kv_free, kv_fork, kv_compact, kv_copy_pages): addresses of the functions of the loaded library
 PyObject* bind_kv(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    void* f[6];
-    if (n != 6) {
-        PyErr_SetString(PyExc_TypeError, "bind_kv takes six addresses");
+    void* f[8];
+    if (n != 8) {
+        PyErr_SetString(PyExc_TypeError, "bind_kv takes eight addresses");
         return nullptr;
     }
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < 8; ++i) {
         f[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
         if (!f[i]) {
-            PyErr_SetString(PyExc_ValueError, "bind_kv takes six addresses");
+            PyErr_SetString(PyExc_ValueError, "bind_kv takes eight addresses");
             return nullptr;
         }
     }
     kv_calls = {(decltype(&::attn_paged))f[0], (decltype(&::kv_append))f[1], (decltype(&::rope))f[2],
-                (decltype(&::kv_reserve))f[3], (decltype(&::kv_free))f[4], (decltype(&::kv_fork))f[5]};
+                (decltype(&::kv_reserve))f[3], (decltype(&::kv_free))f[4], (decltype(&::kv_fork))f[5],
+                (decltype(&::kv_compact))f[6], (decltype(&::kv_copy_pages))f[7]};
     kv_enabled = true;
     Py_RETURN_NONE;
 }
@@ -524,6 +554,8 @@ PyMethodDef methods[] = {
     {"kv_reserve", fast(kv_reserve_), METH_FASTCALL, nullptr},
     {"kv_free", fast(kv_free_), METH_FASTCALL, nullptr},
     {"kv_fork", fast(kv_fork_), METH_FASTCALL, nullptr},
+    {"kv_compact", fast(kv_compact_), METH_FASTCALL, nullptr},
+    {"kv_copy_pages", fast(kv_copy_pages_), METH_FASTCALL, nullptr},
     {"bind", fast(bind), METH_FASTCALL, nullptr},
     {"bind_kv", fast(bind_kv), METH_FASTCALL, nullptr},
     {"disable", disable, METH_NOARGS, nullptr},

@@ -274,11 +274,17 @@ def kv_compact_workspace(pages) -> int:
 
 def kv_compact(k_cache, v_cache, ref, table, kv_len, workspace, stream=None) -> None:
     """Pages in use move to the lowest numbers, with contents, counts and table entries."""
+    rc = _fast().kv_compact(k_cache, v_cache, ref, table, kv_len, workspace, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     _check(_load().kv_compact(_pages(k_cache, v_cache, layers=True), _book(ref, table, kv_len, k_cache.shape[3]), _array(workspace, torch.uint8, "workspace"),
                               workspace.numel(), _stream(stream)))
 
 
 def kv_copy_pages(k_cache, v_cache, src, dst, stream=None) -> None:
     """Pages ``src`` are copied to pages ``dst``, all layers, keys and values."""
+    rc = _fast().kv_copy_pages(k_cache, v_cache, src, dst, stream)
+    if rc is not NotImplemented:
+        return _check(rc)
     n = src.numel()
     _check(_load().kv_copy_pages(_pages(k_cache, v_cache, layers=True), _list(src, n, "src"), _list(dst, n, "dst"), n, _stream(stream)))

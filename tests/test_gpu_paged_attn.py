@@ -305,6 +305,8 @@ def test_with_and_without_the_extension(kv, monkeypatch):
         layers = [dev[x].view(torch.uint8)[None] for x in ("k_cache", "v_cache")]
         kv.kv_fork(*layers, ref, table, kv_len, ints(1), ints(2), missing)
         kv.kv_free(ref, table, kv_len, ints(0), 16)
+        kv.kv_compact(*layers, ref, table, kv_len, torch.empty(kv.kv_compact_workspace(ref.numel()), dtype=torch.uint8, device="cuda"))
+        kv.kv_copy_pages(*layers, ints(0, 1), ints(ref.numel() - 1, ref.numel() - 2))
         torch.cuda.synchronize()
         results.append([q_out, dev["o"], dev["lse"], y, dev["k_cache"].view(torch.uint8), dev["v_cache"].view(torch.uint8), ref, table, kv_len, missing])
         with pytest.raises(kv.KvCacheError) as e:

@@ -209,10 +209,11 @@ def test_what_the_extension_does_not_take():
     from paper_2510_14719_amd import binding
     fast = binding._load_fast()
     x = torch.zeros((3, 2, 64), dtype=torch.float16)
-    for f, n in ((fast.attn_paged, 16), (fast.kv_append, 17), (fast.rope, 8), (fast.kv_reserve, 8), (fast.kv_free, 6), (fast.kv_fork, 9)):
+    for f, n in ((fast.attn_paged, 16), (fast.kv_append, 17), (fast.rope, 8), (fast.kv_reserve, 8), (fast.kv_free, 6), (fast.kv_fork, 9), (fast.kv_compact, 7),
+                 (fast.kv_copy_pages, 5)):
         for args in ([x] * n, [None] * n, [1] * n, [], [x] * (n + 1)):
             assert f(*args) is NotImplemented
     with pytest.raises(TypeError):
         fast.bind_kv(1)
     with pytest.raises(ValueError):
-        fast.bind_kv(0, 0, 0, 0, 0, 0)
+        fast.bind_kv(0, 0, 0, 0, 0, 0, 0, 0)

@@ -494,6 +494,7 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
         const long long tiles = (long long)sequences * p.row_tiles, units = tiles * key_heads, even = (5 << 18) / key_bytes;
         if (units >= 512) {
             if (max_kv > even * 8 / 5) p.split = (int)((even + 127) / 128 * 128);
+            p.splits = (int)((max_kv + p.split - 1) / p.split);
         } else if (max_kv > 1024) {
             // One piece a place, or two or three one after the other where that evens them out (sequences of 9000 of 4 tokens each over E4M3: 37, 32 heads on 4, d 128 115 / 95 us, 20, 128 heads on 16,
             // d 64 106 / 90) and reading the cache takes less time anyway.
@@ -508,16 +509,16 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
                     room = all / key_heads;
                 }
             }
-            if (room > tiles) {                 // (else whole)  The longest sequence may have all pieces that the others leave, or all are alike.
-                const long long least = max_kv / (room - tiles + 1), alike = (max_kv + room / tiles - 1) / (room / tiles);
-                p.split = (int)(least > 512 ? least : 512);
-                p.split_max = (int)(alike > p.split ? alike : p.split);
-                if (sequences == 1 || sequences > 128) p.split = p.split_max;          // (many: finding out would take longer than it saves)
-                if (p.split < p.split_max) p.few_room = (int)room;
-                else if (p.split < whole) p.split = (p.split + 63) / 64 * 64;
+            if (room > tiles) {                 // (else whole)
+                const long long alike = (max_kv + room / tiles - 1) / (room / tiles);
+                p.split = 512;
+                p.split_max = (int)(alike > 512 ? alike : 512);
+                if (sequences > 128) p.split = (p.split_max + 63) / 64 * 64;     // (many: finding out would take longer than it saves)
+                else if (p.split_max > 512) p.few_room = (int)room;
+                p.splits = (int)((max_kv + p.split - 1) / p.split);
+                if (p.few_room > 0 && p.splits > p.few_room) p.splits = p.few_room;
             }
         }
-        p.splits = (int)((max_kv + p.split - 1) / p.split);
     }
     if (!all_small) {
         const long long each = (most + PAGED_CHUNK_ROWS - 1) / PAGED_CHUNK_ROWS * sequences, all = (long long)tokens * group / PAGED_CHUNK_ROWS + sequences;

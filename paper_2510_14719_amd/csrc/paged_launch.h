@@ -24,7 +24,7 @@ struct PagedArgs {
     int heads, group;                                        // query heads, and how many share a key head
     int causal;
     int few_rows;                                            // sequences with more rows (new tokens x group) than this go by chunks of PAGED_CHUNK_ROWS
-    int rows, row_tiles, split, splits;                      // the others: rows per workgroup, row tiles of the longest one, most keys of a piece (a multiple of 128), pieces of
+    int rows, row_tiles, split, splits;                      // the others: rows per workgroup, row tiles of the longest one, most keys of a piece (a multiple of 64), pieces of
                                                              // the longest
     int few_room;                                            // > 0: how long their pieces are is found on the device (few_cut), so that there are at most so many (of every key head)
     float few_finest, few_step, few_coarsest;                // 1 / keys: of the shortest, log2 of a step, of the longest

@@ -134,7 +134,7 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? (i64)p.splits * b->tokens * heads : 0; }
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
-    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.few_room ? 16 : 0);
+    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.splits > 1 ? 16 : 0);
 }
 bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
@@ -257,10 +257,17 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.few_rows = p.few_rows;
     a.rows = p.rows;
     a.row_tiles = p.row_tiles;
-    a.few_room = p.few_room;
+    // Pieces of a fixed length are numbered through on the device too where sequences are far shorter than the bound: that costs 4 us in 200, an empty workgroup 2 ns (one token each of 64
+    // sequences of 300 ... 16384, 32 heads on 8, d 128, bound as it is / 2 / 8 / 32 times that, us numbered 209 / 209 / 210 / 210, else 205 / 206 / 243 / 441).  All tokens lie in
+    // pages, so unless sequences share pages there are no more pieces than this (if they do, the length grows).
+    const i64 row_tiles = (i64)batch->sequences * p.row_tiles, room = row_tiles + p.row_tiles * ((i64)cache->pages * cache->page_size / p.split);
+    const bool fixed = p.splits > 1 && p.few_room == 0 && room * 6 < row_tiles * p.splits;
+    a.few_room = fixed ? (int)room : p.few_room;
+    a.few_fixed = fixed;
     a.few_finest = 1.f / (float)p.split;
-    a.few_coarsest = p.few_room ? 1.f / (float)p.split_max : 0.f;
-    a.few_step = p.few_room ? std::log2((float)p.split_max / (float)p.split) / 63.f : 0.f;
+    const int longest = fixed ? batch->max_kv : p.split_max;
+    a.few_coarsest = a.few_room ? 1.f / (float)longest : 0.f;
+    a.few_step = a.few_room ? std::log2((float)longest / (float)p.split) / 63.f : 0.f;
     a.split = p.split;
     a.splits = p.splits;
     a.chunk_parts = p.chunk_parts;

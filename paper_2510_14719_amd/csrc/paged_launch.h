@@ -27,6 +27,7 @@ struct PagedArgs {
     int rows, row_tiles, split, splits;                      // the others: rows per workgroup, row tiles of the longest one, most keys of a piece (a multiple of 64), pieces of
                                                              // the longest
     int few_room;                                            // > 0: how long their pieces are is found on the device (few_cut), so that there are at most so many (of every key head)
+    int few_fixed;                                           // the shortest length mostly fits
     float few_finest, few_step, few_coarsest;                // 1 / keys: of the shortest, log2 of a step, of the longest
     float* few_inverse;                                      // what was found, for the join
     int chunk_parts;                                         // room for partial results of chunks, in workgroups (0: chunks are not cut along the keys)

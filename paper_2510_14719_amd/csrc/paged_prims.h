@@ -56,6 +56,16 @@ __device__ __forceinline__ SeqRange few_seq(const PagedArgs& a, int s)
 // (`first`: the first 64 sequences, a lane each; a lane has a length)
 __device__ inline float few_cut(const PagedArgs& a, const SeqRange& first, int lane)
 {
+    if (a.few_fixed) {
+        int pieces = 0;
+        for (int s0 = 0; s0 < a.sequences; s0 += 64) {
+            const SeqRange seq = s0 == 0 ? first : few_seq(a, s0 + lane);
+            pieces += few_tiles(a, seq) * few_pieces(a.few_finest, seq.kv);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) pieces += __shfl_xor(pieces, d);
+        if (__builtin_amdgcn_readfirstlane(pieces) <= a.few_room) return a.few_finest;
+    }
     const float inverse = lane == 63 ? a.few_coarsest : a.few_finest * __builtin_amdgcn_exp2f(-a.few_step * lane);
     int pieces = 0;
     for (int s0 = 0; s0 < a.sequences; s0 += 64) {

@@ -100,6 +100,22 @@ def test_pieces_of_sequences_of_all_lengths(kv, count, d, dtype, cache):
     run(kv, Batch(lens, 6, 1, d, dtype, cache, 32, pad=3))
 
 
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("count,d,cache", [(3, 64, "e4m3"), (40, 128, "fp16"), (66, 128, "fp16")])
+def test_bounds_far_from_the_lengths(kv, count, d, cache, shared):
+    """Pieces are numbered through on the device; where sequences share pages there may be more of them than the pages could hold apart."""
+    b = Batch([(1 + i % 2, 5 + 137 * i % 300) for i in range(count)] + [(1, n) for n in (2600, 2561, 2700, 2800, 2900)], 8, 8, d, "fp16", cache, 16)
+    if shared:                                  # every sequence has the last one's first pages
+        used = -(-b.lens[-1][1] // 16)
+        pages = b.table[-1, :used].long()
+        b.k_cache, b.v_cache = (c.view(torch.uint8)[pages].view(c.dtype) for c in (b.k_cache, b.v_cache))
+        for s, (_, n) in enumerate(b.lens):
+            b.table[s, :-(-n // 16)] = torch.arange(-(-n // 16), dtype=torch.int32)
+            b.k[s], b.v[s] = b.k[-1][:n], b.v[-1][:n]
+    b.table = torch.nn.functional.pad(b.table, (0, 29 * b.table.shape[1]), value=-1)
+    run(kv, b, max_kv=30 * b.max_kv)
+
+
 def test_two_calls_at_once(kv):
     """On two streams, each with a workspace of its own."""
     b = Batch([(1, 3000), (2, 2100), (40, 1300)], 4, 2, 128, "bf16", "bf16", 16)

@@ -26,7 +26,7 @@ constexpr float MOVE_LOG2 = 8.0f;               // the reference moves when a ma
 constexpr int NW = 8, BM = PAGED_CHUNK_ROWS, BN = 64, STAGES = 4, QB = 2, KB = BN / 16;
 constexpr int AHEAD = 2;                        // LDS operands requested ahead of their MFMA
 
-template <int DTYPE, bool C8, int D>
+template <int DTYPE, bool C8, int D, bool OWN>
 __global__ __launch_bounds__(NW * 64)
 void attn_paged_chunk(PagedArgs a)
 {
@@ -43,9 +43,19 @@ void attn_paged_chunk(PagedArgs a)
 
     // ---- which chunk, and which piece of its keys
     const int key_heads = a.heads / a.group, h = blockIdx.x % key_heads;
-    const ChunkSeq first = chunk_seq(a, lane);
-    const ChunkCut cut = chunk_cut(a, first, key_heads, lane);
-    const ChunkPiece mine = chunk_numbered(a, first, cut.inverse, blockIdx.x / key_heads, lane);
+    int cut_chunks;                             // how many there are, if they are cut
+    ChunkPiece mine;
+    if constexpr (OWN) {
+        const OwnSeq all = own_seq(a, lane);
+        const OwnCut cut = own_cut(a, all, key_heads, lane);
+        mine = own_numbered(a, all, cut.length, blockIdx.x / key_heads, lane);
+        cut_chunks = cut.chunks;
+    } else {
+        const ChunkSeq first = chunk_seq(a, lane);
+        const ChunkCut cut = chunk_cut(a, first, key_heads, lane);
+        mine = chunk_numbered(a, first, cut.inverse, blockIdx.x / key_heads, lane);
+        cut_chunks = cut.chunks;
+    }
     const int s = __builtin_amdgcn_readfirstlane(mine.s), tile = __builtin_amdgcn_readfirstlane(mine.chunk);
     int keys = 0, per = 0;                      // keys of the chunk, of a piece
     SeqRange seq = {0, 0, 0};
@@ -55,8 +65,8 @@ void attn_paged_chunk(PagedArgs a)
         per = chunk_piece_tiles(mine.pieces, keys) * BN;
     }
     if (threadIdx.x == 0 && a.chunk_parts > 0) {                         // for attn_paged_join_chunks
-        if (blockIdx.x == 0) a.chunk_what[a.chunk_parts * 4] = cut.chunks * key_heads;
-        if (cut.chunks > 0 && s >= 0 && mine.piece == 0)
+        if (blockIdx.x == 0) a.chunk_what[a.chunk_parts * 4] = cut_chunks * key_heads;
+        if (cut_chunks > 0 && s >= 0 && mine.piece == 0)
             *reinterpret_cast<u32x4*>(a.chunk_what + (mine.number * key_heads + h) * 4) =
                 u32x4{(unsigned)s, (unsigned)tile, (unsigned)(per < keys ? (keys + per - 1) / per : 1), blockIdx.x};
     }
@@ -455,17 +465,28 @@ void attn_paged_chunk(PagedArgs a)
     }
 }
 
-template <int DTYPE, bool C8, int D>
-int launch(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
+template <int DTYPE, bool C8, int D, bool OWN>
+int launch_as(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 {
     constexpr int SMEM = STAGES * 2 * CachedRows<D, 2, BN>::BYTES;
-    auto kern = attn_paged_chunk<DTYPE, C8, D>;
+    auto kern = attn_paged_chunk<DTYPE, C8, D, OWN>;
     static PerDeviceOnce once;
     if (once.prepare(reinterpret_cast<const void*>(kern), SMEM) < 0) return -1;
     PagedArgs arg = a;
     void* args[] = {&arg};
     const long long grid = plan.chunk_tiles > a.chunk_parts ? plan.chunk_tiles : a.chunk_parts;
     return hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3((unsigned)grid), dim3(NW * 64), args, SMEM, stream) == hipSuccess ? 0 : -1;
+}
+
+// Whether chunks are cut for the keys that they see themselves: prompts of a few sequences (finding out takes longer the more there are; 6 of up to 1040 tokens, 5 heads on 1, E4M3, d 64 25 us
+// without, 29 with) whose chunks differ and are fewer than the compute units (16 heads, d 128, us without / with: one prompt of 2048 48.7 / 43.3, of 4096, 8 heads 67.3 / 55.9, of 3000, 16 on 2
+// 78.4 / 67.0; two of 1326, 20 on 4, E4M3, d 64 68.7 / 71.4).
+template <int DTYPE, bool C8, int D>
+int launch(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
+{
+    const long long chunks = ((long long)a.max_q * a.group + BM - 1) / BM, all = (long long)a.tokens * a.group / BM + a.sequences, tiles = a.max_kv / 64;
+    const bool own = a.causal && a.chunk_parts > 0 && a.sequences <= OWN_MOST && chunks >= 4 && 16 * (chunks - 1) >= a.group * tiles && (all - a.sequences) * (a.heads / a.group) < a.chunk_parts;
+    return own ? launch_as<DTYPE, C8, D, true>(a, plan, stream) : launch_as<DTYPE, C8, D, false>(a, plan, stream);
 }
 
 }  // namespace

@@ -201,6 +201,85 @@ __device__ inline ChunkPiece chunk_numbered(const PagedArgs& a, const ChunkSeq& 
 // Key tiles per piece.
 __device__ __forceinline__ int chunk_piece_tiles(int pieces, int keys) { return max(1, ((keys + 63) / 64 + pieces - 1) / pieces); }
 
+// ---- the same for prompts, whose chunks see different numbers of keys under the mask: each is cut for its own (see launch)
+struct OwnSeq {
+    int chunks, tiles;                          // chunks of the sequence, key tiles of its last, which are the most
+    float head;                                 // tiles less in the one before that; each further one has 4 / group less
+};
+__device__ __forceinline__ OwnSeq own_seq(const PagedArgs& a, int s)
+{
+    const ChunkSeq q = chunk_seq(a, s);
+    if (q.chunks == 0) return {0, 0, 0.f};
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
+    return {q.chunks, q.tiles, (float)(seq.n * a.group - (q.chunks - 1) * PAGED_CHUNK_ROWS) / (float)(64 * a.group)};
+}
+// Sequence i of those that the lanes have.
+__device__ __forceinline__ OwnSeq own_of(const OwnSeq& q, int i)
+{
+    return {__builtin_amdgcn_readlane(q.chunks, i), __builtin_amdgcn_readlane(q.tiles, i), __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, q.head), i))};
+}
+// How many of the chunks, from the last one on, have more than j pieces when they are cut for so many tiles.
+__device__ __forceinline__ int own_layer(const PagedArgs& a, const OwnSeq& q, float length, int j)
+{
+    if (j == 0) return q.chunks;
+    const float y = __builtin_fmaf(-length, (float)j, (float)q.tiles - 0.01f);
+    if (y <= 0.f) return 0;
+    return 1 + max(0, min(q.chunks - 1, (int)__builtin_fminf(__builtin_ceilf((y - q.head) * (0.25f * a.group)), 1e6f)));
+}
+constexpr float OWN_WHOLE = 1e9f;               // a length that no chunk is cut for
+constexpr int OWN_MOST = 4;                     // sequences of a call, at most
+struct OwnCut {
+    float length;
+    int chunks;
+};
+// (`all`: the sequences, a lane each; a lane has a length.)
+__device__ inline OwnCut own_cut(const PagedArgs& a, const OwnSeq& all, int key_heads, int lane)
+{
+    int longest = 0, chunks = 0;
+    float least = 0.f;                          // tiles of all chunks
+    for (int i = 0; i < a.sequences; ++i) {
+        const OwnSeq q = own_of(all, i);
+        longest = max(longest, q.tiles);
+        chunks += q.chunks;
+        least += (float)(q.chunks * q.tiles) - max(q.chunks - 1, 0) * (q.head + 2.f / a.group * (q.chunks - 2));
+    }
+    if (longest <= CHUNK_UNCUT / 64 || chunks * key_heads >= a.chunk_parts) return {OWN_WHOLE, 0};
+    const float length = (float)longest * __builtin_amdgcn_exp2f(-0.09375f * (1 + lane));
+    const int room = a.chunk_parts / key_heads;
+    // (lengths that are too short are not counted out: a chunk has nearly half a piece more than its tiles make)
+    int pieces = (float)longest - length > CHUNK_SAVES && length >= CHUNK_LEAST && least + 0.4f * length * chunks <= length * room ? 0 : room + 1;
+    for (int i = 0; i < a.sequences; ++i) {
+        const OwnSeq q = own_of(all, i);
+        for (int j = 0, n; pieces <= room && (n = own_layer(a, q, length, j)) > 0; ++j) pieces += n;
+    }
+    const unsigned long long fits = __builtin_amdgcn_ballot_w64(pieces <= room);
+    if (fits == 0) return {OWN_WHOLE, 0};
+    return {__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, length), 63 - __builtin_clzll(fits))), chunks};
+}
+__device__ inline ChunkPiece own_numbered(const PagedArgs& a, const OwnSeq& all, float length, int left, int lane)
+{
+    int number = 0;
+    for (int s = 0; s < a.sequences; ++s) {
+        const OwnSeq q = own_of(all, s);
+        for (int i0 = 0; i0 < q.chunks; i0 += 64) {          // a chunk a lane, the last one first
+            const int i = i0 + lane;
+            int start = 0, pieces = 0;
+            for (int j = 0, n; (n = own_layer(a, q, length, j)) > 0; ++j) {
+                start += min(i, n);
+                pieces += i < n;
+            }
+            const unsigned long long here = __builtin_amdgcn_ballot_w64(start <= left && left < start + pieces);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                return {s, q.chunks - 1 - (i0 + l), left - __builtin_amdgcn_readlane(start, l), __builtin_amdgcn_readlane(pieces, l), number + i0 + l};
+            }
+        }
+        for (int j = 0, n; (n = own_layer(a, q, length, j)) > 0; ++j) left -= n;
+        number += q.chunks;
+    }
+    return {-1, 0, 0, 1, 0};
+}
+
 // Exchange with lane^32 and lane^16: v_permlane32_swap swaps the upper 32 lanes of its first operand with the lower 32 of its second,
 // v_permlane16_swap odd rows of 16 lanes with even ones.  (Inline asm: the compiler folds the two results of the builtins into one when
 // both inputs are the same value; the s_nop covers the VALU-write -> permlane-read hazard.)

@@ -75,6 +75,12 @@ def test_chunks_cut_into_many_pieces(kv, d, dtype, cache, lens):
     run(kv, Batch(lens, 4, 1, d, dtype, cache, 64, peaky=True))
 
 
+@pytest.mark.parametrize("d,dtype,cache", [(128, "bf16", "bf16"), (64, "fp16", "e4m3")])
+@pytest.mark.parametrize("lens", [[(1500, 1500)], [(1301, 1900), (0, 5), (700, 900)], [(1400, 1407), (40, 64), (1, 1), (1030, 1030)]])
+def test_prompts_of_a_few_sequences(kv, d, dtype, cache, lens):
+    run(kv, Batch(lens, 8, 2, d, dtype, cache, 32, pad=3))
+
+
 @pytest.mark.parametrize("d,dtype,cache", [(128, "bf16", "bf16"), (64, "fp16", "fp16"), (128, "fp16", "e4m3")])
 @pytest.mark.parametrize("longest", [1, 32, 33, 64, 129, 224, 225, 256, 257])
 def test_the_shortest_sequences(kv, d, dtype, cache, longest):

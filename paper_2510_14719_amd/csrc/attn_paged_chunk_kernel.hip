@@ -267,7 +267,7 @@ void attn_paged_chunk(PagedArgs a)
     };
     // ---- U of a tile that some row may see in part.  Where it holds values that are not finite, 0 x NaN would be NaN: these stay out of the product and are
     // added key by key to the rows that give them a weight.  (Looking for them costs a wave 16 LDS reads and 140 vector instructions; taking them out
-    // always, 1300 a tile: 256 new tokens of 256, 16 heads, d 128 16.8 us that way, 15.2 so.)
+    // always, 1300 a tile: 256 new tokens of 256, 16 heads, d 128, by chunks 16.8 us that way, 15.2 so.)
     auto careful_u = [&](int j) __attribute__((always_inline)) {
         const char* const vt = stage_ptr(j) + Rows::BYTES;
         const bool care = (j >= nt_full || any_bad) && holds_not_finite<DTYPE, false, Rows::BYTES>(vt, lane);

@@ -114,7 +114,7 @@ __device__ __forceinline__ int few_piece_keys(int pieces, int keys) { return max
 // Chunks of the sequences with more rows than few_rows are numbered through, the last one of a sequence first.  Where they are fewer than the chip has compute
 // units, those of long sequences are cut into pieces; which length to cut for is found on the device, from the lengths that are there, by every wave of the
 // kernel for itself: of 64 lengths, the longest sequence's x 2^(-3c/32), the shortest that still makes no more pieces than there are compute units, if that
-// is worth the joining.  (On MI355X a tile of 64 keys takes 1.6 us, leaving partial results 6, joining them 8.  us cut / not: 12 sequences of 1 ... 777 new tokens,
+// is worth the joining.  (On MI355X a tile of 64 keys takes 1.6 us, leaving partial results 6, joining them 8.  us cut / not, all by chunks: 12 sequences of 1 ... 777 new tokens,
 // 900 ... 4001 keys, 16 heads on 4, d 128 64 / 97 (69 with 15 lengths a fourth of an octave apart); 8 of 64 new tokens, 4000 keys, the same heads 40 / 96; one of 1024, 1024 keys 28 / 34;
 // one of 5, 16384 keys, 32 heads on 4 25 (33 with 16 pieces at most).)
 constexpr int CHUNK_PARTS = 256;                // most pieces: a round of the compute units

@@ -185,7 +185,8 @@ int kv_free(const kv_book *book, const int *list, int n, void *stream);
 /*
  * Row dst[i] becomes a continuation of row src[i], i = 0 ... n - 1: full pages are shared, a last page that is not full is copied to a new one (all
  * layers, keys and values).  What a dst row held before is overwritten, not given back (kv_free does that).  *missing as above: such
- * a row has -1 for its last page.  No row twice in dst, no dst in src.
+ * a row has -1 for its last page.  A page that src does not have (its entry is none, see kv_reserve) dst does not have either: a last one has
+ * -1 there, takes no page and is not counted in *missing.  No row twice in dst, no dst in src.
  */
 int kv_fork(const kv_pages *cache, const kv_book *book, const int *src, const int *dst, int n, int *missing, void *stream);
 

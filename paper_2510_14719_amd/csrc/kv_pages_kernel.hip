@@ -165,14 +165,21 @@ __device__ __forceinline__ void copy_page(const PageCopy& c, char* base, int lay
     }
 }
 
+// Whether row s has a last page that is not full and is there.  (Where it is not, the continuation has none either: a page given out in its place would show
+// what its last owner left in it.)
+__device__ __forceinline__ bool has_part(const kv_book& b, int s)
+{
+    const int len = tokens_of(b, b.kv_len[s]);
+    return len % b.page_size > 0 && (unsigned)b.table[(long long)s * b.table_stride + len / b.page_size] < (unsigned)b.pages;
+}
+
 __global__ __launch_bounds__(PLAN)
 void fork_plan_kernel(kv_book b, const int* src, const int* dst, int n, int* missing)
 {
     extern __shared__ int before[];
     sum_list(before, n, [&](int i) {
         const int s = src[i], d = dst[i];
-        if ((unsigned)s >= (unsigned)b.rows || (unsigned)d >= (unsigned)b.rows || s == d) return 0;
-        return tokens_of(b, b.kv_len[s]) % b.page_size > 0 ? 1 : 0;
+        return (unsigned)s < (unsigned)b.rows && (unsigned)d < (unsigned)b.rows && s != d && has_part(b, s) ? 1 : 0;
     });
     const int want = before[n];
     auto place = [&](int k) -> int& {
@@ -193,7 +200,8 @@ void fork_kernel(PageCopy c, kv_book b, const int* src, const int* dst, int part
 {
     const int s = src[blockIdx.y], d = dst[blockIdx.y];
     if ((unsigned)s >= (unsigned)b.rows || (unsigned)d >= (unsigned)b.rows || s == d) return;
-    const int len = tokens_of(b, b.kv_len[s]), full = len / b.page_size, part = len % b.page_size > 0;
+    const int len = tokens_of(b, b.kv_len[s]), full = len / b.page_size;
+    const bool part = has_part(b, s);
     const int* const from = b.table + (long long)s * b.table_stride;
     int* const to = b.table + (long long)d * b.table_stride;
     if (blockIdx.x == 0) {
@@ -208,7 +216,7 @@ void fork_kernel(PageCopy c, kv_book b, const int* src, const int* dst, int part
     }
     if (!part) return;
     const int old = from[full], now = to[full];
-    if ((unsigned)old >= (unsigned)b.pages || (unsigned)now >= (unsigned)b.pages) return;
+    if ((unsigned)now >= (unsigned)b.pages) return;
     int id = blockIdx.x - 1;
     const int p = id % parts;
     id /= parts;

@@ -130,8 +130,9 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 {
     return paged_plan(b->sequences, b->tokens, max_q_of(b), b->max_kv, heads, c->heads, c->d, c->dtype == KV_E4M3 ? 1 : 2);
 }
-// Rows of partial results, d + 2 floats each (O, reference and sum): of the small tiles, and of the chunks.
-i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? (i64)p.splits * b->tokens * heads : 0; }
+// Rows of partial results, d + 2 floats each (O, reference and sum): of the small tiles, and of the chunks.  An even number, so that what stands behind them, which is read
+// 16 bytes at a time, begins at a multiple of 16.
+i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? ((i64)p.splits * b->tokens * heads + 1) / 2 * 2 : 0; }
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
     return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.splits > 1 ? 16 : 0);

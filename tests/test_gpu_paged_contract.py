@@ -5,7 +5,7 @@ import random
 import pytest
 import torch
 
-from tests.paged_util import Batch, workspace_for
+from tests.paged_util import Batch, check, workspace_for
 from tests.test_gpu_kv_pages import Model, ints
 
 pytestmark = pytest.mark.gpu
@@ -89,3 +89,17 @@ def test_a_continuation_sees_what_its_source_sees(kv, cache):
     torch.cuda.synchronize()
     assert table.tolist()[1] == table.tolist()[0][:2] + [-1] and missing.tolist() == [0] and kv_len.tolist() == [40, 40] and int(ref.sum()) == 4
     assert math.isfinite(float(dev["o"].float().abs().sum())) and torch.equal(dev["o"][2:], dev["o"][:2]) and torch.equal(dev["lse"][2:], dev["lse"][:2])
+
+
+@pytest.mark.parametrize("d,dtype,cache", [(128, "bf16", "bf16"), (64, "fp16", "e4m3")])
+def test_an_odd_number_of_partial_results_beside_chunks(kv, d, dtype, cache):
+    """65 sequences, an odd number of tokens and one head: small tiles, cut chunks and the lists of both in one workspace."""
+    lens = [(1, 2500)] + [(1, 1 + 7 * i % 60) for i in range(62)] + [(100, 2400), (40, 1300)]
+    b = Batch(lens, 1, 1, d, dtype, cache, 16)
+    b.max_kv = 2503                             # (five pieces of 512, and 203 tokens)
+    dev = b.cuda()
+    dev["table"] = torch.nn.functional.pad(dev["table"], (0, 1), value=-1)
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], dev["lse"], b.max_q, b.max_kv, 1 / math.sqrt(d),
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), b.max_q, b.max_kv), **dev["scales"])
+    torch.cuda.synchronize()
+    check(dev["o"], dev["lse"], b.reference(1 / math.sqrt(d), True))

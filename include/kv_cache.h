@@ -90,7 +90,8 @@ typedef struct kv_rows {
  * Keys and values that a row does not see have no influence on it, NaN and infinities among them; a NaN in a key or value that it sees
  * makes the row NaN (in the value: the features that have one), unless the key's weight is zero in float32 for that row.
  * Scores, maxima and sums are float32; the weights are rounded to `dtype` for the product with V (values up to 2^8 relative to a
- * reference inside the row), an E4M3 cache is widened to `dtype` without rounding.
+ * reference inside the row) and O is divided by the sum of the rounded ones, so it is a mean of the values; the LSE is that of the weights before rounding.  An E4M3
+ * cache is widened to `dtype` without rounding.
  *   workspace   attn_paged_workspace bytes, 16-byte aligned (NULL if that is 0); need not be initialised.
  */
 int attn_paged(const kv_pages *cache, const kv_batch *batch, const kv_rows *q, const kv_rows *o, float *lse, int heads, float scale, int causal,

@@ -232,11 +232,16 @@ void attn_paged_chunk(PagedArgs a)
     f32x4 O[FB][QB], S[KB][QB];
     u32x4 pw[KB / 2][QB];
     float m_run[QB], neg_mc[QB], L[QB];
+    // Sums of the rounded weights, from the matrix cores: the first element.  (4096 new tokens of 16384, 32 heads on 8, d 128, us: without them 778, so 781 ... 799, with vector instructions
+    // 825; d 64, 4096 of 8192: 234 / 242 / 272.)
+    f32x4 R[QB];
+    const s16x8 ones = all_ones<DTYPE>();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         m_run[qb] = m_none;
         neg_mc[qb] = -m_none * c;
         L[qb] = 0.f;
+        R[qb] = f32x4(0.f);
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb) O[fb][qb] = f32x4(0.f);
     }
@@ -255,6 +260,10 @@ void attn_paged_chunk(PagedArgs a)
         for (int f = 0; f < NF; ++f) {
             if (f + AHEAD < NF) fetch(f + AHEAD);
             if (f < NU) {
+                if (f % FB == FB - 1) {
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) R[qb] = E::mfma16(ones, __builtin_bit_cast(s16x8, pw[f / FB][qb]), R[qb]);
+                }
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) O[f % FB][qb] = E::mfma16(fr[f], __builtin_bit_cast(s16x8, pw[f / FB][qb]), O[f % FB][qb]);
             } else {
@@ -271,6 +280,10 @@ void attn_paged_chunk(PagedArgs a)
     auto careful_u = [&](int j) __attribute__((always_inline)) {
         const char* const vt = stage_ptr(j) + Rows::BYTES;
         const bool care = (j >= nt_full || any_bad) && holds_not_finite<DTYPE, false, Rows::BYTES>(vt, lane);
+#pragma unroll
+        for (int kc = 0; kc < KB / 2; ++kc)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) R[qb] = E::mfma16(ones, __builtin_bit_cast(s16x8, pw[kc][qb]), R[qb]);
 #pragma unroll
         for (int kc = 0; kc < KB / 2; ++kc)
 #pragma unroll
@@ -342,6 +355,7 @@ void attn_paged_chunk(PagedArgs a)
                 neg_mc[qb] = -m_run[qb] * c;
                 const float alpha = __builtin_amdgcn_exp2f((m_old - m_run[qb]) * c);
                 L[qb] *= alpha;
+                R[qb][0] *= alpha;
 #pragma unroll
                 for (int fb = 0; fb < FB; ++fb) O[fb][qb] = O[fb][qb] * alpha;
             }
@@ -448,7 +462,7 @@ void attn_paged_chunk(PagedArgs a)
         if (tok >= seq.n) continue;
         const long long row = (long long)t * a.heads + head;
         if (whole) {
-            const float inv = (L[qb] == 0.f ? 0.f : 1.f / L[qb]) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+            const float inv = (R[qb][0] == 0.f ? 0.f : 1.f / R[qb][0]) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
             char* const to = a.o + t * a.o_token + head * a.o_head + lg * 8;
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
@@ -460,7 +474,7 @@ void attn_paged_chunk(PagedArgs a)
             const long long at = (long long)blockIdx.x * BM + r % BM;
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(a.chunk_o + at * D + fb * 16 + lg * 4) = O[fb][qb];
-            if (lg == 0) *reinterpret_cast<f32x2*>(a.chunk_ml + at * 2) = f32x2{m_run[qb] * c, L[qb]};
+            if (lg == 0) *reinterpret_cast<f32x4*>(a.chunk_ml + at * 4) = f32x4{m_run[qb] * c, L[qb], R[qb][0], 0.f};
         }
     }
 }

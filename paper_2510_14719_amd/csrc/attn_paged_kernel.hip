@@ -27,8 +27,7 @@ template <int D, int ES, int QB> struct FewLayout {
     typedef CachedRows<D, ES, 32> Rows;
     static constexpr int STAGE = 2 * Rows::BYTES, SLOTS = 2;
     static constexpr int JOIN = NW * (D / 16) * QB * 1024;   // O of every wave
-    static constexpr int SUMS = 1024;                        // first: reference and sum of every wave's rows
-    static_assert(NW * QB * 16 * 8 <= SUMS);
+    static constexpr int SUMS = NW * QB * 16 * 16;           // first: reference and sums of every wave's rows
     static constexpr int smem(int stages) { return SUMS + (stages * STAGE > JOIN ? stages * STAGE : JOIN); }
 };
 
@@ -102,12 +101,17 @@ void attn_paged_few(PagedArgs a)
     // first keys are hidden.)
     const float m_none = c > 1.f ? -0x1.fffff0p127f / c : -__FLT_MAX__;
     f32x4 O[FB][QB];
+    // Sums of the weights: as they are, for the LSE, and as the product with V takes them, rounded, for O (see paged_prims.h).  The latter comes from the matrix cores,
+    // a block of ones in the place of V^T; its first element is read.
     float m_run[QB], neg_mc[QB], L[QB];
+    f32x4 R[QB];
+    const s16x8 ones = all_ones<DTYPE>();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         m_run[qb] = m_none;
         neg_mc[qb] = -m_none * c;
         L[qb] = 0.f;
+        R[qb] = f32x4(0.f);
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb) O[fb][qb] = f32x4(0.f);
     }
@@ -214,6 +218,7 @@ void attn_paged_few(PagedArgs a)
                 neg_mc[qb] = -m_run[qb] * c;
                 const float alpha = __builtin_amdgcn_exp2f((m_old - m_run[qb]) * c);
                 L[qb] *= alpha;
+                R[qb][0] *= alpha;
 #pragma unroll
                 for (int fb = 0; fb < FB; ++fb) O[fb][qb] = O[fb][qb] * alpha;
             }
@@ -226,6 +231,7 @@ void attn_paged_few(PagedArgs a)
                 }
 #pragma unroll
             for (int t = 0; t < 4; ++t) P[qb][t] = E::pack2(S[t / 2][qb][t % 2 * 2], S[t / 2][qb][t % 2 * 2 + 1]);
+            R[qb] = E::mfma16(ones, __builtin_bit_cast(s16x8, P[qb]), R[qb]);
         }
         if (!masked || !holds_not_finite<DTYPE, C8, Rows::BYTES>(vt, lane)) {
 #pragma unroll
@@ -281,27 +287,28 @@ void attn_paged_few(PagedArgs a)
         L[qb] = groups_sum(L[qb]);
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb) *reinterpret_cast<f32x4*>(join + ((wave * FB + fb) * QB + qb) * 1024 + lane * 16) = O[fb][qb];
-        if (lg == 0) *reinterpret_cast<f32x2*>(sums + ((wave * QB + qb) * 16 + lc) * 2) = f32x2{m_run[qb], L[qb]};
+        if (lg == 0) *reinterpret_cast<f32x4*>(sums + ((wave * QB + qb) * 16 + lc) * 4) = f32x4{m_run[qb], L[qb], R[qb][0], 0.f};
     }
     __syncthreads();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        f32x2 ml[NW];
-        float m = m_none, l = 0.f, w[NW];
+        f32x4 ml[NW];
+        float m = m_none, l = 0.f, rounded = 0.f, w[NW];
 #pragma unroll
         for (int v = 0; v < NW; ++v) {
-            ml[v] = *reinterpret_cast<const f32x2*>(sums + ((v * QB + qb) * 16 + lc) * 2);
+            ml[v] = *reinterpret_cast<const f32x4*>(sums + ((v * QB + qb) * 16 + lc) * 4);
             m = __builtin_fmaxf(m, ml[v][0]);
         }
 #pragma unroll
         for (int v = 0; v < NW; ++v) {
             w[v] = __builtin_amdgcn_exp2f((ml[v][0] - m) * c);
             l += ml[v][1] * w[v];
+            rounded += ml[v][2] * w[v];
         }
         const bool real = o_row[qb] >= 0;
         const int t = real ? (int)(o_row[qb] / a.heads) : 0, head = real ? (int)(o_row[qb] % a.heads) : 0;
         const long long at = (long long)sp * a.tokens * a.heads + o_row[qb];
-        const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+        const float inv = (rounded == 0.f ? 0.f : 1.f / rounded) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
 #pragma unroll
         for (int f = 0; f < FB / NW; ++f) {
             const int fb = wave * (FB / NW) + f;
@@ -317,7 +324,7 @@ void attn_paged_few(PagedArgs a)
             }
         }
         if (real && wave == 0 && lg == 0) {
-            if (!whole) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m * c, l};
+            if (!whole) *reinterpret_cast<f32x4*>(a.part_ml + at * 4) = f32x4{m * c, l, rounded, 0.f};
             else if (a.lse) a.lse[o_row[qb]] = m * scale + __builtin_logf(l);
         }
     }
@@ -332,7 +339,7 @@ void attn_paged_join(PagedArgs a)
     typedef Elem<DTYPE> E;
     constexpr int LANES = D / 4, GROUPS = WAVES * 64 / LANES;
     __shared__ f32x4 s_x[GROUPS][LANES];
-    __shared__ float s_l[GROUPS];
+    __shared__ f32x2 s_l[GROUPS];
     const int lane = threadIdx.x & 63, group = threadIdx.x / LANES, e = threadIdx.x % LANES;
     // the r-th row of key head h of sequence s
     const int key_heads = a.heads / a.group, most = min(a.row_tiles * a.rows, a.max_q * a.group), r = blockIdx.x % most, h = blockIdx.x / most % key_heads;
@@ -344,19 +351,19 @@ void attn_paged_join(PagedArgs a)
     const int n = (keys + per - 1) / per, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
     const long long row = (long long)t * a.heads + head, all = (long long)a.tokens * a.heads;
     const float* const part_o = a.part_o + row * D;
-    const float* const part_ml = a.part_ml + row * 2;
+    const float* const part_ml = a.part_ml + row * 4;
     float m = -__builtin_inff();
-    for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, part_ml[i * all * 2]);
+    for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, part_ml[i * all * 4]);
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, i));
     // (every part has a finite reference, so m is finite)
     f32x4 x = f32x4(0.f);
-    float l = 0.f;
+    f32x2 l = f32x2(0.f);                       // of the weights, and of the rounded ones
 #pragma unroll 4
     for (int i = group; i < n; i += GROUPS) {
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(part_ml + i * all * 2);
+        const f32x4 ml = *reinterpret_cast<const f32x4*>(part_ml + i * all * 4);
         const float w = __builtin_amdgcn_exp2f(ml[0] - m);
-        l += ml[1] * w;
+        l += f32x2{ml[1], ml[2]} * w;
         x += *reinterpret_cast<const f32x4*>(part_o + i * all * D + e * 4) * w;
     }
     s_x[group][e] = x;
@@ -368,9 +375,9 @@ void attn_paged_join(PagedArgs a)
         x += s_x[g][e];
         l += s_l[g];
     }
-    const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+    const float inv = (l[1] == 0.f ? 0.f : 1.f / l[1]) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
     *reinterpret_cast<u32x2*>(a.o + t * a.o_token + head * a.o_head + e * 8) = u32x2{E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};
-    if (a.lse && e == 0) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    if (a.lse && e == 0) a.lse[row] = (m + __builtin_amdgcn_logf(l[0])) * 0.6931471805599453f;
 }
 
 // ---- the pieces of a chunk joined: D / 4 lanes a row, so 1024 / D rows by a workgroup
@@ -391,17 +398,17 @@ void attn_paged_join_chunks(PagedArgs a)
     if (tok >= seq.n) return;
     const long long first = (long long)what[3] * PAGED_CHUNK_ROWS + r;
     const int lane = threadIdx.x & 15;          // 16 lanes have 16 pieces' references and sums
-    f32x2 ml = *reinterpret_cast<const f32x2*>(a.chunk_ml + (first + min(lane, n - 1) * step) * 2);
+    f32x4 ml = *reinterpret_cast<const f32x4*>(a.chunk_ml + (first + min(lane, n - 1) * step) * 4);
     float m = ml[0];
-    for (int k = 16 + lane; k < n; k += 16) m = __builtin_fmaxf(m, a.chunk_ml[(first + k * step) * 2]);
+    for (int k = 16 + lane; k < n; k += 16) m = __builtin_fmaxf(m, a.chunk_ml[(first + k * step) * 4]);
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d));
-    float l = 0.f;
+    f32x2 l = f32x2(0.f);                       // of the weights, and of the rounded ones
     f32x4 x = f32x4(0.f);
     for (int k = 0; k < n; k += 16) {
-        if (k > 0) ml = *reinterpret_cast<const f32x2*>(a.chunk_ml + (first + min(k + lane, n - 1) * step) * 2);
+        if (k > 0) ml = *reinterpret_cast<const f32x4*>(a.chunk_ml + (first + min(k + lane, n - 1) * step) * 4);
         const float w = __builtin_amdgcn_exp2f(ml[0] - m);
-        l += k + lane < n ? ml[1] * w : 0.f;
+        l += k + lane < n ? f32x2{ml[1], ml[2]} * w : f32x2(0.f);
         const int some = min(16, n - k);
         auto add = [&](auto count, int j) __attribute__((always_inline)) {       // so many loads under way
 #pragma unroll
@@ -415,11 +422,11 @@ void attn_paged_join_chunks(PagedArgs a)
         if (j < some) add(std::integral_constant<int, 2>(), j);
     }
 #pragma unroll
-    for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
+    for (int d = 1; d < 16; d *= 2) l += f32x2{__shfl_xor(l[0], d), __shfl_xor(l[1], d)};
     const int t = seq.q0 + tok;
-    const float inv = (l == 0.f ? 0.f : 1.f / l) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
+    const float inv = (l[1] == 0.f ? 0.f : 1.f / l[1]) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
     *reinterpret_cast<u32x2*>(a.o + t * a.o_token + head * a.o_head + e * 8) = u32x2{E::pack2(x[0] * inv, x[1] * inv), E::pack2(x[2] * inv, x[3] * inv)};
-    if (a.lse && e == 0) a.lse[(long long)t * a.heads + head] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    if (a.lse && e == 0) a.lse[(long long)t * a.heads + head] = (m + __builtin_amdgcn_logf(l[0])) * 0.6931471805599453f;
 }
 
 template <int DTYPE, bool C8, int D, int QB>
@@ -475,7 +482,7 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
     auto workgroups = [&](int rows) { return (double)((most + rows - 1) / rows) * sequences * key_heads; };
     auto places = [&](int rows, int kv) {       // what the LDS and the registers hold on 256 compute units
         const int stages = kv < 256 ? (kv + 31) / 32 : 8;
-        const long long ring = stages * 32 * key_bytes, join = rows * d * 16, fit = (160 << 10) / (1024 + (ring > join ? ring : join)), regs = rows == 32 ? (d == 128 ? 1 : 2) : d == 128 ? 2 : cache_bytes == 2 ? 3 : 4;
+        const long long ring = stages * 32 * key_bytes, join = rows * d * 16, fit = (160 << 10) / (rows * 64 + (ring > join ? ring : join)), regs = rows == 32 ? (d == 128 ? 1 : 2) : d == 128 ? 2 : cache_bytes == 2 ? 3 : 4;
         return 256 * (fit < regs ? fit : regs);
     };
     const double small = workgroups(32), chip = places(16, 256);

@@ -130,12 +130,12 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 {
     return paged_plan(b->sequences, b->tokens, max_q_of(b), b->max_kv, heads, c->heads, c->d, c->dtype == KV_E4M3 ? 1 : 2);
 }
-// Rows of partial results, d + 2 floats each (O, reference and sum): of the small tiles, and of the chunks.  An even number, so that what stands behind them, which is read
-// 16 bytes at a time, begins at a multiple of 16.
-i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? ((i64)p.splits * b->tokens * heads + 1) / 2 * 2 : 0; }
+// Rows of partial results, d + 4 floats each (O, reference, two sums, padding: a multiple of 16 bytes, as what stands behind them is read 16 bytes at a time): of the
+// small tiles, and of the chunks.
+i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? (i64)p.splits * b->tokens * heads : 0; }
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
-    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 2) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.splits > 1 ? 16 : 0);
+    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 4) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.splits > 1 ? 16 : 0);
 }
 bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
@@ -242,8 +242,8 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.part_o = (float*)workspace;
     a.chunk_o = a.part_o + few * cache->d;
     a.part_ml = a.chunk_o + chunk * cache->d;
-    a.chunk_ml = a.part_ml + few * 2;
-    a.chunk_what = (int*)(a.chunk_ml + chunk * 2);
+    a.chunk_ml = a.part_ml + few * 4;
+    a.chunk_what = (int*)(a.chunk_ml + chunk * 4);
     a.few_inverse = (float*)(a.chunk_what + (p.chunk_parts ? (p.chunk_parts + 1) * 4 : 0));
     a.sequences = batch->sequences;
     a.tokens = batch->tokens;

@@ -19,7 +19,7 @@ struct PagedArgs {
     char* o;
     float* lse;
     long long q_token, q_head, o_token, o_head;              // strides, bytes
-    float *part_o, *part_ml;                                 // partial results: [split][token * heads + head][d], [..][2]
+    float *part_o, *part_ml;                                 // partial results: [split][token * heads + head][d], [..][4]: reference, sum of the weights, of the rounded ones
     int sequences, tokens, table_stride, max_q, max_kv, pages, page_shift;
     int heads, group;                                        // query heads, and how many share a key head
     int causal;
@@ -31,7 +31,7 @@ struct PagedArgs {
     float few_finest, few_step, few_coarsest;                // 1 / keys: of the shortest, log2 of a step, of the longest
     float* few_inverse;                                      // what was found, for the join
     int chunk_parts;                                         // room for partial results of chunks, in workgroups (0: chunks are not cut along the keys)
-    float *chunk_o, *chunk_ml;                               // [workgroup][PAGED_CHUNK_ROWS][d], [..][2]
+    float *chunk_o, *chunk_ml;                               // [workgroup][PAGED_CHUNK_ROWS][d], [..][4]
     int* chunk_what;                                         // [chunk of a key head][4]: sequence, chunk in it, pieces, workgroup of the first; behind the last [..][0] their number
     float scale;
 };

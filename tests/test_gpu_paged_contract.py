@@ -5,7 +5,7 @@ import random
 import pytest
 import torch
 
-from tests.paged_util import Batch, check, workspace_for
+from tests.paged_util import HALF_STEP, Batch, check, workspace_for
 from tests.test_gpu_kv_pages import Model, ints
 
 pytestmark = pytest.mark.gpu
@@ -103,3 +103,42 @@ def test_an_odd_number_of_partial_results_beside_chunks(kv, d, dtype, cache):
                   workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), b.max_q, b.max_kv), **dev["scales"])
     torch.cuda.synchronize()
     check(dev["o"], dev["lse"], b.reference(1 / math.sqrt(d), True))
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("lens,H,Hk,d", [
+    ([(64, 64)], 4, 2, 64), ([(1, 700), (3, 90), (1, 5000)], 16, 2, 128),         # small tiles, whole and in pieces
+    ([(2100, 2100)], 16, 16, 128), ([(64, 4000)] * 8, 16, 4, 128),                # chunks, whole and in pieces
+])
+def test_a_row_is_a_mean_of_its_values(kv, lens, H, Hk, d, dtype, cache):
+    """Values are in 1 ... 1 + w.  A weight p rounded to the type is off by u p at most (u half a step; in fp16 by 2^-25 of the largest, too), so the mean with
+    rounded weights, divided by THEIR sum, is off by (u + n 2^-25) w; scores that are off by delta change weights by 2 delta p; the result is rounded, half a step u of values in 1 ... 2.
+    (Divided by the sum of the weights as they are it would be off by another u, 16 or 8 times as much.)  Scores have a standard deviation of 2, so few keys have a say."""
+    b = Batch(lens, H, Hk, d, dtype, cache, 16)
+    g = torch.Generator().manual_seed(3)
+    width = 1 / 8 if cache == "e4m3" else 1 / 16
+    dev = b.cuda()
+    for s, (_, n) in enumerate(lens):           # (values of the type itself, so that they are what the reference has)
+        b.v[s] = (1 + width * torch.randint(0, 2 if cache == "e4m3" else 9, (n, Hk, d), generator=g) / (1 if cache == "e4m3" else 8)).to(b.cache_dtype)
+        at = torch.arange(n)
+        page, slot = b.table[s].long()[at // 16].cuda(), (at % 16).cuda()
+        dev["v_cache"].view(torch.uint8).unflatten(-1, (d, -1))[page, :, slot] = b.v[s].cuda().view(torch.uint8).unflatten(-1, (d, -1))
+    scales = {"k_scale": b.k_scale.cuda(), "v_scale": torch.ones(Hk, device="cuda")} if cache == "e4m3" else {}
+    scale = 2 / math.sqrt(d)
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], None, b.max_q, b.max_kv, scale,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), b.max_q, b.max_kv), **scales)
+    u = HALF_STEP[b.dtype]
+    for s, (m, n) in enumerate(lens):
+        t0 = int(b.q_start[s])
+        for h in range(H):
+            q, k, v = b.q[t0:t0 + m, h].cuda().double(), b.k[s][:, h // (H // Hk)].cuda().double(), b.v[s][:, h // (H // Hk)].cuda().double()
+            if cache == "e4m3":
+                k = k * float(b.k_scale[h // (H // Hk)])
+            x = scale * (q @ k.t().contiguous())
+            x.masked_fill_(torch.arange(n, device="cuda")[None] > (n - m + torch.arange(m, device="cuda"))[:, None], -math.inf)
+            want = x.softmax(-1) @ v
+            # (scores: d products in fp32, and three roundings of the exponent)
+            delta = (d + 2) * 2.0 ** -24 * scale * float(q.norm(dim=1).max() * k.norm(dim=1).max()) + 6 * 2.0 ** -24 * float(x[x > -math.inf].abs().max()) + 2.0 ** -21
+            bound = u + (1 + u) * ((u + n * 2.0 ** -25 + 2 * delta) * width + n * 2.0 ** -23)
+            err = float((dev["o"][t0:t0 + m, h].double() - want).abs().max())
+            assert err <= bound, "sequence %d, head %d: %.3e, %.3f of the bound" % (s, h, err, err / bound)

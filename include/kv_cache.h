@@ -65,7 +65,8 @@ typedef struct kv_pages {
  *   q_start      int32 [sequences + 1], not falling, 0 ... tokens.       kv_len   int32 [sequences].
  *   table        int32 [sequences][table_width], rows table_stride entries apart: page of the tokens j * page_size ... of a sequence.
  *   max_q        no sequence has more new tokens than this; max_kv: none is longer.  max_kv <= table_width * page_size.
- * Both bounds choose the launch (a tight one is faster); a sequence beyond them is cut off.
+ * Both bounds choose the launch (a tight one is faster).  Of a sequence beyond them, the first max_q new tokens and those at positions below max_kv are worked on, at the
+ * positions that they have; the rest counts neither as tokens nor as keys, and its rows are left as they are in every output.
  */
 typedef struct kv_batch {
     const int *q_start, *kv_len, *table;

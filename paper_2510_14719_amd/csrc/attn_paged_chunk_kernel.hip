@@ -58,10 +58,10 @@ void attn_paged_chunk(PagedArgs a)
     }
     const int s = __builtin_amdgcn_readfirstlane(mine.s), tile = __builtin_amdgcn_readfirstlane(mine.chunk);
     int keys = 0, per = 0;                      // keys of the chunk, of a piece
-    SeqRange seq = {0, 0, 0};
+    SeqRange seq = {0, 0, 0, 0};
     if (s >= 0) {
         seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
-        keys = __builtin_amdgcn_readfirstlane(paged_tile_keys(tile, BM, seq.n, a.group, seq.kv, a.causal));
+        keys = __builtin_amdgcn_readfirstlane(paged_tile_keys(tile, BM, seq.n, a.group, seq.first, seq.kv, a.causal));
         per = chunk_piece_tiles(mine.pieces, keys) * BN;
     }
     if (threadIdx.x == 0 && a.chunk_parts > 0) {                         // for attn_paged_join_chunks
@@ -87,14 +87,14 @@ void attn_paged_chunk(PagedArgs a)
         const char* const at = a.q + t * a.q_token + head * a.q_head + lg * 16;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) Qf[qb][kk] = *reinterpret_cast<const s16x8*>(at + kk * 64);
-        last_key[qb] = a.causal ? min(seq.kv - seq.n + tok, keys - 1) : keys - 1;
+        last_key[qb] = a.causal ? min(seq.first + tok, keys - 1) : keys - 1;
     }
     // keys of the split that any row of this wave sees, and those that all of them see, in tiles
     int nt = (k1 - k0 + BN - 1) / BN, nt_w, nt_full;
     {
         const int first_tok = wq0 / a.group, last_tok = min((wq0 + QB * 16 - 1) / a.group, seq.n - 1);
-        const int w_end = first_tok >= seq.n ? 0 : a.causal ? min(k1, seq.kv - seq.n + last_tok + 1) : k1;
-        const int w_all = a.causal ? min(k1, seq.kv - seq.n + first_tok + 1) : k1;
+        const int w_end = first_tok >= seq.n ? 0 : a.causal ? min(k1, seq.first + last_tok + 1) : k1;
+        const int w_all = a.causal ? min(k1, seq.first + first_tok + 1) : k1;
         nt = max(nt, 0);
         nt_w = w_end > k0 ? (w_end - k0 + BN - 1) / BN : 0;
         nt_full = w_all > k0 ? min((w_all - k0) / BN, nt_w) : 0;

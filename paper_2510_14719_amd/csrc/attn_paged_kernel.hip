@@ -64,9 +64,9 @@ void attn_paged_few(PagedArgs a)
         mine.seq = seq_range(a.q_start, a.kv_len, mine.s, a.tokens, a.max_q, a.max_kv);
     }
     const int s = __builtin_amdgcn_readfirstlane(mine.s), tile = __builtin_amdgcn_readfirstlane(mine.tile), sp = __builtin_amdgcn_readfirstlane(mine.piece);
-    const SeqRange seq = {__builtin_amdgcn_readfirstlane(mine.seq.q0), __builtin_amdgcn_readfirstlane(mine.seq.n), __builtin_amdgcn_readfirstlane(mine.seq.kv)};
+    const SeqRange seq = {__builtin_amdgcn_readfirstlane(mine.seq.q0), __builtin_amdgcn_readfirstlane(mine.seq.n), __builtin_amdgcn_readfirstlane(mine.seq.kv), __builtin_amdgcn_readfirstlane(mine.seq.first)};
     if (tile * ROWS >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.kv, a.causal), per = a.few_room > 0 ? few_piece_keys(mine.pieces, keys) : paged_piece_keys(keys, a.split);
+    const int keys = paged_tile_keys(tile, ROWS, seq.n, a.group, seq.first, seq.kv, a.causal), per = a.few_room > 0 ? few_piece_keys(mine.pieces, keys) : paged_piece_keys(keys, a.split);
     const int k0 = sp * per, k1 = min(keys, k0 + per);
     if (sp > 0 && k0 >= keys) return;
     const bool whole = keys <= per;
@@ -91,10 +91,10 @@ void attn_paged_few(PagedArgs a)
         const char* const at = a.q + t * a.q_token + head * a.q_head + lg * 16;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) Qf[qb][kk] = *reinterpret_cast<const s16x8*>(at + kk * 64);
-        last_key[qb] = a.causal ? min(seq.kv - seq.n + tok, keys - 1) : keys - 1;
+        last_key[qb] = a.causal ? min(seq.first + tok, keys - 1) : keys - 1;
         o_row[qb] = real ? (long long)t * a.heads + head : -1;
     }
-    const int first_last = a.causal ? seq.kv - seq.n + tile * ROWS / a.group : keys - 1;   // what the first row sees
+    const int first_last = a.causal ? seq.first + tile * ROWS / a.group : keys - 1;   // what the first row sees
 
     const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
     // The reference before the first score: the most negative float whose scaled value is finite.  (-inf would make NaN of rows whose
@@ -345,7 +345,7 @@ void attn_paged_join(PagedArgs a)
     const int key_heads = a.heads / a.group, most = min(a.row_tiles * a.rows, a.max_q * a.group), r = blockIdx.x % most, h = blockIdx.x / most % key_heads;
     const SeqRange seq = seq_range(a.q_start, a.kv_len, blockIdx.x / most / key_heads, a.tokens, a.max_q, a.max_kv);
     if (r >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
-    const int keys = paged_tile_keys(r / a.rows, a.rows, seq.n, a.group, seq.kv, a.causal);
+    const int keys = paged_tile_keys(r / a.rows, a.rows, seq.n, a.group, seq.first, seq.kv, a.causal);
     const int per = a.few_room > 0 ? few_piece_keys(few_pieces(*a.few_inverse, seq.kv), keys) : paged_piece_keys(keys, a.split);
     if (keys <= per) return;
     const int n = (keys + per - 1) / per, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;

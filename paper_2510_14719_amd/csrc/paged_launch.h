@@ -45,13 +45,13 @@ struct PagedPlan {
 };
 PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads, int key_heads, int d, int cache_bytes);
 
-// Row tiles as they are cut from a sequence: tile t has the rows t * rows ... of the n * group rows (token-major) of its n new tokens.
-// Keys that its rows may see, and in how many splits.
-PAGED_HD inline int paged_tile_keys(int tile, int rows, int n, int group, int kv, int causal)
+// Row tiles as they are cut from a sequence: tile t has the rows t * rows ... of the n * group rows (token-major) of its n new tokens, the first of which has position `first`.
+// How many of its kv keys the rows of a tile may see.
+PAGED_HD inline int paged_tile_keys(int tile, int rows, int n, int group, int first, int kv, int causal)
 {
     if (!causal) return kv;
     const int last = (tile + 1) * rows - 1, token = last / group;
-    const int end = kv - n + (token < n ? token : n - 1) + 1;
+    const int end = first + (token < n ? token : n - 1) + 1;
     return end < 0 ? 0 : end;
 }
 

@@ -9,14 +9,17 @@
 
 namespace {
 
-// New tokens and length of a sequence, brought into the bounds of the call whatever the arrays hold.
+// New tokens of a sequence, what it has in all and the position of its first new token, brought into the bounds of the call whatever the arrays hold: of too many new tokens the
+// first max_q are left, of a sequence that is too long those at positions below max_kv.  Both keep their positions (negative where there are more new tokens than tokens).
 struct SeqRange {
-    int q0, n, kv;
+    int q0, n, kv, first;
 };
 __device__ __forceinline__ SeqRange seq_range(const int* q_start, const int* kv_len, int s, int tokens, int max_q, int max_kv)
 {
-    const int q0 = min(max(q_start[s], 0), tokens), q1 = min(max(q_start[s + 1], q0), tokens);
-    return {q0, min(q1 - q0, max_q), min(max(kv_len[s], 0), max_kv)};
+    const int q0 = min(max(q_start[s], 0), tokens), all = min(max(q_start[s + 1], q0), tokens) - q0, first = max(kv_len[s], 0) - all;
+    int n = min(all, max_q);
+    if (first > max_kv - n) n = max(max_kv - first, 0);
+    return {q0, n, min(max(first + n, 0), max_kv), first};
 }
 
 // The last sequence that starts at or before token t, found by the 64 lanes of a wave together (two steps up to 4096 sequences);
@@ -51,7 +54,7 @@ __device__ __forceinline__ int few_tiles(const PagedArgs& a, const SeqRange& seq
 }
 __device__ __forceinline__ SeqRange few_seq(const PagedArgs& a, int s)
 {
-    return s < a.sequences ? seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv) : SeqRange{0, 0, 0};
+    return s < a.sequences ? seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv) : SeqRange{0, 0, 0, 0};
 }
 // (`first`: the first 64 sequences, a lane each; a lane has a length)
 __device__ inline float few_cut(const PagedArgs& a, const SeqRange& first, int lane)
@@ -100,11 +103,12 @@ __device__ inline FewPiece few_numbered(const PagedArgs& a, const SeqRange& firs
         const unsigned long long beyond = __builtin_amdgcn_ballot_w64(sum > left);
         if (beyond) {
             const int at = __builtin_ctzll(beyond), n = __builtin_amdgcn_readlane(pieces, at), inside = left - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(own, at));
-            return {s0 + at, inside / n, inside % n, n, {__builtin_amdgcn_readlane(seq.q0, at), __builtin_amdgcn_readlane(seq.n, at), __builtin_amdgcn_readlane(seq.kv, at)}};
+            return {s0 + at, inside / n, inside % n, n, 
+                    {__builtin_amdgcn_readlane(seq.q0, at), __builtin_amdgcn_readlane(seq.n, at), __builtin_amdgcn_readlane(seq.kv, at), __builtin_amdgcn_readlane(seq.first, at)}};
         }
         left -= __builtin_amdgcn_readlane(sum, 63);
     }
-    return {-1, 0, 0, 1, {0, 0, 0}};
+    return {-1, 0, 0, 1, {0, 0, 0, 0}};
 }
 // Keys of a piece of a row tile with so many keys.
 __device__ __forceinline__ int few_piece_keys(int pieces, int keys) { return max(((keys + pieces - 1) / pieces + 63) / 64 * 64, 64); }

@@ -173,7 +173,7 @@ void kv_append_kernel(AppendArgs a, int log_tokens)
         if (s >= 0) {
             const SeqRange seq = seq_range(a.q_start, a.kv_len, s, a.tokens, a.max_q, a.max_kv);
             real = t >= seq.q0 && t - seq.q0 < seq.n;
-            pos = seq.kv - seq.n + (t - seq.q0);
+            pos = seq.first + (t - seq.q0);
             if (real && pos >= 0) {
                 const int page = a.table[(long long)s * a.table_stride + (pos >> a.page_shift)];
                 if ((unsigned)page < (unsigned)a.pages) place = page * a.page_bytes + (pos & ((1 << a.page_shift) - 1)) * a.token_bytes;

@@ -1,7 +1,9 @@
 """What the header promises of the operators around a paged cache where pages, lengths or values are not as they should be."""
+import copy
 import math
 import random
 
+import numpy as np
 import pytest
 import torch
 
@@ -142,3 +144,72 @@ def test_a_row_is_a_mean_of_its_values(kv, lens, H, Hk, d, dtype, cache):
             bound = u + (1 + u) * ((u + n * 2.0 ** -25 + 2 * delta) * width + n * 2.0 ** -23)
             err = float((dev["o"][t0:t0 + m, h].double() - want).abs().max())
             assert err <= bound, "sequence %d, head %d: %.3e, %.3f of the bound" % (s, h, err, err / bound)
+
+
+SHORT = [(5, 40), (2, 9), (7, 30), (10, 5), (1, 36)]
+MIXED = [(1 + i % 4, 8 + 7 * i % 90) for i in range(150)]
+for at, long in ((3, (40, 1500)), (64, (20, 900)), (70, (70, 70)), (127, (9, 1100)), (149, (36, 1499))):
+    MIXED[at] = long
+CUT = [(SHORT, 3, 40), (SHORT, 10, 36), (SHORT, 4, 28), (SHORT, 1, 1), ([(6, 3000), (3, 1200), (1, 5)], 4, 2998), (MIXED, 33, 1496)]
+
+
+def cut_lens(lens, max_q, max_kv):
+    """What is left of (new tokens, all tokens) of each sequence: the first max_q new ones, at positions below max_kv."""
+    out = []
+    for n, kv in lens:
+        first = kv - n
+        m = max(0, min(n, max_q, max_kv - first))
+        out.append((m, max(0, min(first + m, max_kv))))
+    return out
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,max_q,max_kv", CUT)
+def test_attention_of_sequences_beyond_the_bounds(kv, lens, max_q, max_kv, causal):
+    b = Batch(lens, 4, 1, 64, "fp16", "fp16", 16, pad=2)
+    dev = b.cuda()
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], dev["lse"], max_q, max_kv, 1 / 8, causal,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), max_q, max_kv))
+    torch.cuda.synchronize()
+    want = copy.copy(b)
+    want.lens = cut_lens(lens, max_q, max_kv)
+    # (the token of a sequence whose new tokens outnumber it has a negative position: it sees nothing with the mask, and what there is without)
+    seen = want.seen
+
+    def at_its_position(s, causal):
+        ok = seen(s, causal)
+        if causal:
+            first = lens[s][1] - lens[s][0]
+            ok &= np.arange(ok.shape[1])[None] <= (first + np.arange(ok.shape[0]))[:, None]
+        return ok
+    want.seen = at_its_position
+    check(dev["o"], dev["lse"], want.reference(1 / 8, causal))
+
+
+@pytest.mark.parametrize("cache", ["fp16", "e4m3"])
+@pytest.mark.parametrize("lens,max_q,max_kv", CUT)
+def test_append_of_sequences_beyond_the_bounds(kv, lens, max_q, max_kv, cache):
+    """The tokens that are left get the places and angles that they have in the whole call; nothing else is written."""
+    b = Batch(lens, 4, 2, 64, "fp16", cache, 16, pad=2)
+    g = torch.Generator().manual_seed(4)
+    k, v = (torch.randn((b.tokens, 2, 64), generator=g).half().cuda() for _ in "kv")
+    freq = kv.rope_frequencies(64).cuda()
+    results = []
+    for bounds in ((b.max_q, b.max_kv), (max_q, max_kv)):
+        dev = b.cuda()
+        q_out = torch.full_like(dev["q"], 55.0)
+        kv.kv_append(k, v, dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], *bounds, q=dev["q"], q_out=q_out, freq=freq, **dev["scales"])
+        results.append((dev["k_cache"].view(torch.uint8).cpu(), dev["v_cache"].view(torch.uint8).cpu(), q_out.cpu()))
+    before = [b.k_cache.view(torch.uint8), b.v_cache.view(torch.uint8)]
+    for i in range(2):                          # a place of a token that is left as in the whole call, others as before
+        want = before[i].clone()
+        for s, (m, _) in enumerate(cut_lens(lens, max_q, max_kv)):
+            for pos in range(max(0, lens[s][1] - lens[s][0]), lens[s][1] - lens[s][0] + m):
+                page = int(b.table[s, pos // 16])
+                want[page, :, pos % 16] = results[0][i][page, :, pos % 16]
+        assert torch.equal(results[1][i], want)
+    q_want = torch.full_like(results[0][2], 55.0)
+    for s, (m, _) in enumerate(cut_lens(lens, max_q, max_kv)):
+        t0 = int(b.q_start[s])
+        q_want[t0:t0 + m] = results[0][2][t0:t0 + m]
+    assert torch.equal(results[1][2], q_want)

@@ -70,6 +70,7 @@ void attn_paged_few(PagedArgs a)
     const int k0 = sp * per, k1 = min(keys, k0 + per);
     if (sp > 0 && k0 >= keys) return;
     const bool whole = keys <= per;
+    if (a.few_first && sp == 0 && h == 0 && threadIdx.x == 0) a.few_first[s * a.row_tiles + tile] = blockIdx.x / key_heads;
 
     // ---- the wave's steps are 32 keys each, every NW-th of the piece's
     const int* const table = a.table + (long long)s * a.table_stride;
@@ -307,7 +308,9 @@ void attn_paged_few(PagedArgs a)
         }
         const bool real = o_row[qb] >= 0;
         const int t = real ? (int)(o_row[qb] / a.heads) : 0, head = real ? (int)(o_row[qb] % a.heads) : 0;
-        const long long at = (long long)sp * a.tokens * a.heads + o_row[qb];
+        const int r = tile * ROWS + qb * 16 + lc;
+        const long long at = a.few_first ? (long long)blockIdx.x * ROWS + qb * 16 + lc
+                                         : sp * a.part_rows + (a.part_most > 0 ? ((long long)s * key_heads + h) * a.part_most + r : o_row[qb]);
         const float inv = (rounded == 0.f ? 0.f : 1.f / rounded) * (C8 && a.v_scale ? a.v_scale[h] : 1.f);
 #pragma unroll
         for (int f = 0; f < FB / NW; ++f) {
@@ -343,15 +346,20 @@ void attn_paged_join(PagedArgs a)
     const int lane = threadIdx.x & 63, group = threadIdx.x / LANES, e = threadIdx.x % LANES;
     // the r-th row of key head h of sequence s
     const int key_heads = a.heads / a.group, most = min(a.row_tiles * a.rows, a.max_q * a.group), r = blockIdx.x % most, h = blockIdx.x / most % key_heads;
-    const SeqRange seq = seq_range(a.q_start, a.kv_len, blockIdx.x / most / key_heads, a.tokens, a.max_q, a.max_kv);
+    const long long sequence = blockIdx.x / most / key_heads;
+    const int first = a.few_first ? a.few_first[sequence * a.row_tiles + r / a.rows] : 0;      // (on its way under what follows; of a tile without pieces anything)
+    const SeqRange seq = seq_range(a.q_start, a.kv_len, (int)sequence, a.tokens, a.max_q, a.max_kv);
     if (r >= seq.n * a.group || seq.n * a.group > a.few_rows) return;
     const int keys = paged_tile_keys(r / a.rows, a.rows, seq.n, a.group, seq.first, seq.kv, a.causal);
     const int per = a.few_room > 0 ? few_piece_keys(few_pieces(*a.few_inverse, seq.kv), keys) : paged_piece_keys(keys, a.split);
     if (keys <= per) return;
     const int n = (keys + per - 1) / per, t = seq.q0 + r / a.group, head = h * a.group + r % a.group;
-    const long long row = (long long)t * a.heads + head, all = (long long)a.tokens * a.heads;
-    const float* const part_o = a.part_o + row * D;
-    const float* const part_ml = a.part_ml + row * 4;
+    const long long row = (long long)t * a.heads + head;
+    const long long all = a.few_first ? (long long)key_heads * a.rows : a.part_rows;                 // slots from a piece to the next
+    const long long slot = a.few_first ? ((long long)first * key_heads + h) * a.rows + r % a.rows
+                         : a.part_most > 0 ? (sequence * key_heads + h) * a.part_most + r : row;
+    const float* const part_o = a.part_o + slot * D;
+    const float* const part_ml = a.part_ml + slot * 4;
     float m = -__builtin_inff();
     for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, part_ml[i * all * 4]);
 #pragma unroll

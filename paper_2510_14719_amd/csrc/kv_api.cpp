@@ -130,12 +130,24 @@ PagedPlan plan_of(const kv_pages* c, const kv_batch* b, int heads)
 {
     return paged_plan(b->sequences, b->tokens, max_q_of(b), b->max_kv, heads, c->heads, c->d, c->dtype == KV_E4M3 ? 1 : 2);
 }
-// Rows of partial results, d + 4 floats each (O, reference, two sums, padding: a multiple of 16 bytes, as what stands behind them is read 16 bytes at a time): of the
-// small tiles, and of the chunks.
-i64 few_parts(const PagedPlan& p, const kv_batch* b, int heads) { return p.splits > 1 ? (i64)p.splits * b->tokens * heads : 0; }
+// Partial results of the small tiles (see PagedArgs): d + 4 floats a slot (O, reference, two sums, padding: a multiple of 16 bytes, as what stands behind them is read
+// 16 bytes at a time).  Sequences that go by chunks have none of them, however many tokens they have.
+struct FewParts {
+    i64 rows, slots;
+    int most;                                   // as PagedArgs::part_most
+};
+FewParts few_parts(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
+{
+    if (p.splits <= 1) return {0, 0, 0};
+    if (p.few_room > 0) return {0, (i64)p.few_room * c->heads * p.rows, 0};
+    const i64 rows = (i64)max_q_of(b) * (heads / c->heads), tiles = (i64)p.row_tiles * p.rows, most = rows < tiles ? rows : tiles;
+    const i64 by_token = (i64)b->tokens * heads, by_sequence = (i64)b->sequences * c->heads * most;
+    return by_sequence < by_token ? FewParts{by_sequence, by_sequence * p.splits, (int)most} : FewParts{by_token, by_token * p.splits, 0};
+}
+i64 few_first_bytes(const PagedPlan& p, const kv_batch* b) { return p.splits > 1 && p.few_room > 0 ? ((i64)b->sequences * p.row_tiles + 3) / 4 * 16 : 0; }
 i64 workspace_of(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
-    return (few_parts(p, b, heads) + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 4) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.splits > 1 ? 16 : 0);
+    return (few_parts(p, c, b, heads).slots + (i64)p.chunk_parts * PAGED_CHUNK_ROWS) * (c->d + 4) * 4 + (p.chunk_parts ? (p.chunk_parts + 1) * 16ll : 0) + (p.splits > 1 ? 16 : 0) + few_first_bytes(p, b);
 }
 bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads)
 {
@@ -238,13 +250,17 @@ int attn_paged(const kv_pages* cache, const kv_batch* batch, const kv_rows* q, c
     a.q_head = q->head_stride * 2;
     a.o_token = o->token_stride * 2;
     a.o_head = o->head_stride * 2;
-    const i64 few = few_parts(p, batch, heads), chunk = (i64)p.chunk_parts * PAGED_CHUNK_ROWS;
+    const FewParts parts = few_parts(p, cache, batch, heads);
+    const i64 few = parts.slots, chunk = (i64)p.chunk_parts * PAGED_CHUNK_ROWS;
     a.part_o = (float*)workspace;
     a.chunk_o = a.part_o + few * cache->d;
     a.part_ml = a.chunk_o + chunk * cache->d;
     a.chunk_ml = a.part_ml + few * 4;
     a.chunk_what = (int*)(a.chunk_ml + chunk * 4);
     a.few_inverse = (float*)(a.chunk_what + (p.chunk_parts ? (p.chunk_parts + 1) * 4 : 0));
+    a.part_rows = parts.rows;
+    a.part_most = parts.most;
+    a.few_first = few_first_bytes(p, batch) > 0 ? (int*)(a.few_inverse + 4) : nullptr;
     a.sequences = batch->sequences;
     a.tokens = batch->tokens;
     a.table_stride = batch->table_stride;

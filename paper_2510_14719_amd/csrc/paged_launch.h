@@ -19,7 +19,13 @@ struct PagedArgs {
     char* o;
     float* lse;
     long long q_token, q_head, o_token, o_head;              // strides, bytes
-    float *part_o, *part_ml;                                 // partial results: [split][token * heads + head][d], [..][4]: reference, sum of the weights, of the rounded ones
+    // Partial results of the small tiles, [slot][d] and [slot][4]: reference, sum of the weights, of the rounded ones.  A slot is a row of a piece.
+    // Where pieces are numbered from the plan on (few_first), piece i of key head h has the slots (i * key heads + h) * rows ...; else piece p of a row has the slot
+    // p * part_rows + its row, counted as token * heads + head, or, where those are fewer (part_most > 0), as the r-th of part_most of its sequence and key head.
+    float *part_o, *part_ml;
+    long long part_rows;
+    int part_most;
+    int* few_first;                                          // [sequence][row tile]: number of its first piece
     int sequences, tokens, table_stride, max_q, max_kv, pages, page_shift;
     int heads, group;                                        // query heads, and how many share a key head
     int causal;

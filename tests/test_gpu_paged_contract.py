@@ -150,7 +150,7 @@ SHORT = [(5, 40), (2, 9), (7, 30), (10, 5), (1, 36)]
 MIXED = [(1 + i % 4, 8 + 7 * i % 90) for i in range(150)]
 for at, long in ((3, (40, 1500)), (64, (20, 900)), (70, (70, 70)), (127, (9, 1100)), (149, (36, 1499))):
     MIXED[at] = long
-CUT = [(SHORT, 3, 40), (SHORT, 10, 36), (SHORT, 4, 28), (SHORT, 1, 1), ([(6, 3000), (3, 1200), (1, 5)], 4, 2998), (MIXED, 33, 1496)]
+CUT = [(SHORT, 3, 40), (SHORT, 10, 36), (SHORT, 4, 28), (SHORT, 1, 1), ([(6, 3000), (3, 1200), (1, 5)], 4, 2996), (MIXED, 33, 1496)]
 
 
 def cut_lens(lens, max_q, max_kv):
@@ -213,3 +213,19 @@ def test_append_of_sequences_beyond_the_bounds(kv, lens, max_q, max_kv, cache):
         t0 = int(b.q_start[s])
         q_want[t0:t0 + m] = results[0][2][t0:t0 + m]
     assert torch.equal(results[1][2], q_want)
+
+
+@pytest.mark.parametrize("loose", [1, 12])
+def test_pieces_beside_many_prompts(kv, loose):
+    """Sequences of up to 32 rows are cut in a batch that has far more tokens than they have rows, with bounds that are tight and that are not."""
+    lens = [(40, 45)] * 130
+    for at, some in ((0, (3, 4500)), (33, (20, 4200)), (65, (1, 9)), (129, (32, 4497))):
+        lens[at] = some
+    b = Batch(lens, 4, 4, 128, "bf16", "bf16", 16, pad=1)
+    dev = b.cuda()
+    dev["table"] = torch.nn.functional.pad(dev["table"], (0, (loose - 1) * dev["table"].shape[1]), value=-1)
+    workspace = workspace_for(kv, dev["q"], dev["k_cache"], 130, 40, 4500 * loose)
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], dev["lse"], 40, 4500 * loose, 1 / math.sqrt(128),
+                  workspace=workspace)
+    torch.cuda.synchronize()
+    check(dev["o"], dev["lse"], b.reference(1 / math.sqrt(128), True))

@@ -89,7 +89,7 @@ typedef struct kv_rows {
  *   lse    float32 [tokens][heads], written; NULL: not wanted.
  * Layer 0 of the cache is read (a caller with several points k and v at the one it means).
  * Keys and values that a row does not see have no influence on it, NaN and infinities among them; a NaN in a key or value that it sees
- * makes the row NaN (in the value: the features that have one), unless the key's weight is zero in float32 for that row.
+ * makes the row NaN (in the value: the features that have one) and an infinity in a value makes the feature NaN or infinite, whatever the key's weight.
  * Scores, maxima and sums are float32; the weights are rounded to `dtype` for the product with V (values up to 2^8 relative to a
  * reference inside the row) and O is divided by the sum of the rounded ones, so it is a mean of the values; the LSE is that of the weights before rounding.  An E4M3
  * cache is widened to `dtype` without rounding.

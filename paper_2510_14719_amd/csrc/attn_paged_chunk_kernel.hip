@@ -274,8 +274,18 @@ void attn_paged_chunk(PagedArgs a)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // The 16-key blocks of a tile that lie in no page.
+    auto no_pages = [&](int j) __attribute__((always_inline)) {
+        unsigned bad = 0;
+        if (any_bad) {
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+                bad |= (unsigned)__builtin_amdgcn_readfirstlane(table[min(k0 + j * BN + b * 16, keys - 1) >> a.page_shift]) >= (unsigned)a.pages ? 1u << b : 0u;
+        }
+        return bad;
+    };
     // ---- U of a tile that some row may see in part.  Where it holds values that are not finite, 0 x NaN would be NaN: these stay out of the product and are
-    // added key by key to the rows that give them a weight.  (Looking for them costs a wave 16 LDS reads and 140 vector instructions; taking them out
+    // added key by key to the rows that see them, whatever their weight, as the product does where every row sees every key.  (Looking for them costs a wave 16 LDS reads and 140 vector instructions; taking them out
     // always, 1300 a tile: 256 new tokens of 256, 16 heads, d 128, by chunks 16.8 us that way, 15.2 so.)
     auto careful_u = [&](int j) __attribute__((always_inline)) {
         const char* const vt = stage_ptr(j) + Rows::BYTES;
@@ -297,10 +307,13 @@ void attn_paged_chunk(PagedArgs a)
                 for (int qb = 0; qb < QB; ++qb) O[fb][qb] = E::mfma16(__builtin_bit_cast(s16x8, w), __builtin_bit_cast(s16x8, pw[kc][qb]), O[fb][qb]);
             }
         if (!care) return;
+        const unsigned bad = no_pages(j);
         for (int k = 0; k < BN; ++k) {
             float p[QB];
+            bool seen[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
+                seen[qb] = k0 + j * BN + k <= last_key[qb] && !((bad >> (k >> 4)) & 1);
                 unsigned x = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x = (k >> 3 & 4) + (k >> 1 & 3) == e ? pw[e / 4][qb][e % 4] : x;
@@ -313,7 +326,7 @@ void attn_paged_chunk(PagedArgs a)
                 for (int i = 0; i < 4; ++i) {
                     const float x = Rows::template v_value<DTYPE>(vt, k, fb * 16 + lg * 4 + i);
 #pragma unroll
-                    for (int qb = 0; qb < QB; ++qb) O[fb][qb][i] += __builtin_isfinite(x) || p[qb] == 0.f ? 0.f : p[qb] * x;
+                    for (int qb = 0; qb < QB; ++qb) O[fb][qb][i] += __builtin_isfinite(x) || !seen[qb] ? 0.f : p[qb] * x;
                 }
         }
     };
@@ -322,12 +335,7 @@ void attn_paged_chunk(PagedArgs a)
     auto softmax_tile = [&](int j, auto masked) __attribute__((always_inline)) {
         if (decltype(masked)::value) {
             const int key0 = k0 + j * BN;
-            unsigned bad = 0;                   // 16-key blocks in no page
-            if (any_bad) {
-#pragma unroll
-                for (int b = 0; b < KB; ++b)
-                    bad |= (unsigned)__builtin_amdgcn_readfirstlane(table[min(key0 + b * 16, keys - 1) >> a.page_shift]) >= (unsigned)a.pages ? 1u << b : 0u;
-            }
+            const unsigned bad = no_pages(j);
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
 #pragma unroll

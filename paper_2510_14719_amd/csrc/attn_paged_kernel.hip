@@ -243,7 +243,7 @@ void attn_paged_few(PagedArgs a)
             }
         } else {
             // Where some row does not see some key, 0 x NaN would be NaN: there, values that are not finite stay out of the product and
-            // are added key by key to the rows that give them a weight.
+            // are added key by key to the rows that see them, whatever their weight, as the product does where every row sees every key.
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
                 u32x4 w = __builtin_bit_cast(u32x4, Rows::template v_operand<DTYPE>(vt, 0, fb, lane));
@@ -254,8 +254,10 @@ void attn_paged_few(PagedArgs a)
             }
             for (int j = 0; j < 32; ++j) {
                 float p[QB];
+                bool seen[QB];
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
+                    seen[qb] = key + j <= last_key[qb] && !((bad >> (j >> 4)) & 1);
                     float x = S[0][qb][0];
 #pragma unroll
                     for (int e = 1; e < 8; ++e) x = (j & 7) == e ? S[e / 4][qb][e % 4] : x;
@@ -267,7 +269,7 @@ void attn_paged_few(PagedArgs a)
                     for (int i = 0; i < 4; ++i) {
                         const float x = Rows::template v_value<DTYPE>(vt, j, fb * 16 + lg * 4 + i);
 #pragma unroll
-                        for (int qb = 0; qb < QB; ++qb) O[fb][qb][i] += __builtin_isfinite(x) || p[qb] == 0.f ? 0.f : p[qb] * x;
+                        for (int qb = 0; qb < QB; ++qb) O[fb][qb][i] += __builtin_isfinite(x) || !seen[qb] ? 0.f : p[qb] * x;
                     }
             }
         }

@@ -229,3 +229,44 @@ def test_pieces_beside_many_prompts(kv, loose):
                   workspace=workspace)
     torch.cuda.synchronize()
     check(dev["o"], dev["lse"], b.reference(1 / math.sqrt(128), True))
+
+
+@pytest.mark.parametrize("down", [2.5, 20.0])
+@pytest.mark.parametrize("lens,H,Hk,d,cache,value", [(*case, value) for case in (
+    ([(6, 200), (1, 40), (3, 3)], 4, 2, 64, "fp16"), ([(6, 2000), (2, 40)], 4, 2, 128, "e4m3"), ([(64, 4000)] * 8, 16, 4, 128, "fp16"), ([(2100, 2100)], 16, 16, 128, "e4m3"))
+    for value in ((math.nan,) if case[-1] == "e4m3" else (math.nan, math.inf, -math.inf))])       # (E4M3 has no infinities)
+def test_values_that_are_not_finite_show_whatever_their_weight(kv, lens, H, Hk, d, cache, down, value):
+    """Keys are 0 but for three, which score -scale d down = -20 and -160: weights of 2e-9, nothing in fp16, and of nothing in float32.  One of them all rows see in a whole
+    tile, one only some, one is the newest.  Values are 1, so O is 1 where no row sees what is not finite."""
+    b = Batch(lens, H, Hk, d, "fp16", cache, 16)
+    b.k_scale = b.v_scale = None
+    dev = b.cuda()
+    dev["q"].fill_(1.0)
+    features = {}                               # (sequence, key) -> feature
+    for s, (n, m) in enumerate(lens):
+        for i, key in enumerate({3, max(0, m - 1 - n // 2), m - 1}):
+            features[s, key] = i
+    for s, (n, m) in enumerate(lens):
+        k, v = torch.zeros((m, Hk, d)), torch.ones((m, Hk, d))
+        for (seq, key), f in features.items():
+            if seq == s and key < m:
+                k[key] = -down
+                v[key, :, f] = value
+        at = torch.arange(m)
+        page, slot = b.table[s].long()[at // 16].cuda(), (at % 16).cuda()
+        for name, x in (("k_cache", k), ("v_cache", v)):
+            dev[name].view(torch.uint8).unflatten(-1, (d, -1))[page, :, slot] = x.to(b.cache_dtype).cuda().view(torch.uint8).unflatten(-1, (d, -1))
+    scale = 8 / d
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], None, b.max_q, b.max_kv, scale,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), b.max_q, b.max_kv))
+    o = dev["o"].float().cpu()
+    for s, (n, m) in enumerate(lens):
+        t0 = int(b.q_start[s])
+        shows = torch.zeros((n, d), dtype=torch.bool)
+        for (seq, key), f in features.items():
+            if seq == s and key < m:
+                shows[:, f] |= m - n + torch.arange(n) >= key
+        x, shows = o[t0:t0 + n], shows[:, None].expand(n, H, d)
+        assert not x[shows].isfinite().any() and (not math.isnan(value) or x[shows].isnan().all())
+        # (the weights are alike: a mean of ones is off by the sums' rounding, m 2^-24, and the result's)
+        assert ((x[~shows] - 1).abs() <= m * 2.0 ** -23 + 2.0 ** -11).all()

@@ -178,6 +178,9 @@ enum { KV_MAX_LIST = 8192 };
  * Room for growth: row list[i] gets pages for new_len[i] tokens in all (entries behind those it holds, in the order of the list and then of the
  * tokens) and kv_len = new_len[i]; a row that is as long already stays as it is.  What is longer than the table is cut to its width.
  * *missing is the number of pages that were not there: their entries are -1.  No row twice in a list.
+ * kv_len counts the tokens of missing pages all the same (kv_append passes over them, attention sees nothing there), and an entry that was missing stays so: later calls
+ * begin behind what kv_len counts, for a page given out there would show what its last owner left in it.  Such a row is given back and begun anew, or, before it
+ * grows again and before anything is appended to it, its kv_len is set to page_size x the entries that it has (the missing ones are its last) and the call made again.
  */
 int kv_reserve(const kv_book *book, const int *list, const int *new_len, int n, int *missing, void *stream);
 

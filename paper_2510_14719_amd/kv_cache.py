@@ -239,7 +239,10 @@ def _list(x, n, what):
 
 
 def kv_reserve(ref, table, kv_len, rows, new_len, missing, page_size, stream=None) -> None:
-    """Rows get pages for ``new_len`` tokens in all, lowest free page first; ``missing`` int32 [1]: how many were not there."""
+    """Rows get pages for ``new_len`` tokens in all, lowest free page first; ``missing`` int32 [1]: how many were not there.
+
+    Their entries are -1 and stay so, though ``kv_len`` counts the tokens: after a call that missed pages give them back (``kv_free``), or set the ``kv_len`` of
+    the rows to ``page_size`` times the entries that they have and call again."""
     rc = _fast().kv_reserve(ref, table, kv_len, rows, new_len, missing, page_size, stream)
     if rc is not NotImplemented:
         return _check(rc)

@@ -270,3 +270,24 @@ def test_values_that_are_not_finite_show_whatever_their_weight(kv, lens, H, Hk, 
         assert not x[shows].isfinite().any() and (not math.isnan(value) or x[shows].isnan().all())
         # (the weights are alike: a mean of ones is off by the sums' rounding, m 2^-24, and the result's)
         assert ((x[~shows] - 1).abs() <= m * 2.0 ** -23 + 2.0 ** -11).all()
+
+
+def test_a_row_with_missing_pages_is_taken_up_again(kv):
+    """As the header says: another call alone fills nothing; with kv_len set back to what the row has, it does, and no page is lost."""
+    m = Pages(1, 6, 1, 16, 64, torch.float16, 3, 5, "head")
+    for rows, lens, missing in (([0], [40], 0), ([1, 2], [30, 70], 4)):
+        assert m.reserve(rows, lens) == missing
+        kv.kv_reserve(*m.dev, ints(rows), ints(lens), m.missing, 16)
+        m.check("reserve", missing)
+    m.release([0])
+    kv.kv_free(*m.dev, ints([0]), 16)
+    assert m.reserve([2], [70]) == 0
+    kv.kv_reserve(*m.dev, ints([2]), ints([70]), m.missing, 16)
+    m.check("the same again", 0)
+    assert m.table[2][:5] == [5, -1, -1, -1, -1]
+    m.len[2] = 16
+    m.dev[2][2] = 16
+    assert m.reserve([2], [70]) == 1
+    kv.kv_reserve(*m.dev, ints([2]), ints([70]), m.missing, 16)
+    m.check("taken up", 1)
+    assert m.table[2][:5] == [5, 0, 1, 2, -1] and m.ref == [1] * 6

@@ -171,7 +171,7 @@ typedef struct kv_book {
     int pages, rows, table_width, table_stride, page_size;
 } kv_book;
 
-/* Most rows in one list. */
+/* Most rows in one list (of kv_reserve also: rows x table_width below 2^31, so that the pages wanted can be counted). */
 enum { KV_MAX_LIST = 8192 };
 
 /*

@@ -450,6 +450,7 @@ int kv_reserve(const kv_book* book, const int* list, const int* new_len, int n, 
     if ((rc = check_list(list, n)) != KV_OK || (rc = check_list(new_len, n)) != KV_OK) return rc;
     if (!missing) return KV_ERR_NULL;
     if (misaligned(missing, 4)) return KV_ERR_ALIGN;
+    if ((i64)n * book->table_width >= (1ll << 31)) return KV_ERR_OVERFLOW;       // (wants are counted in 32 bits)
     return launched(kv_reserve_launch(*book, list, new_len, n, missing, stream));
 }
 

@@ -31,7 +31,7 @@ enum {
     KV_ERR_ALIGN = -4,      /* a pointer or a stride is not aligned */
     KV_ERR_OVERFLOW = -5,   /* too large for the kernels' index arithmetic or for a grid */
     KV_ERR_LAUNCH = -6,     /* the HIP runtime refused a launch */
-    KV_ERR_ALIAS = -7,      /* an output overlaps an input or another output */
+    KV_ERR_ALIAS = -7,      /* an output (a workspace, a book that is changed) overlaps an input (arrays of a batch, lists, scales too) or another output */
     KV_ERR_STRIDE = -8,     /* a stride is smaller than a row, so rows would overlap */
     KV_ERR_WORKSPACE = -9   /* the workspace is smaller than the call needs */
 };
@@ -46,7 +46,8 @@ enum { KV_HALF = 0, KV_INTERLEAVED = 1 };
  * A cache.  Element e of token t of page p, head h, layer l stands at
  *     l * layer_stride + p * page_stride + h * head_stride + t * token_stride + e        (in elements, for k and for v alike)
  * from k or v, so any order of the dimensions is a matter of the strides.  Rows (d elements) must not overlap; every stride of a
- * dimension larger than one is >= d, k and v are 16-byte aligned and strides are multiples of 16 bytes.
+ * dimension larger than one is >= d, k and v are 16-byte aligned and strides are multiples of 16 bytes.  Where the cache is written, rows of k and of v must not
+ * meet either; they may lie between each other where every stride steps over all that lies inside it.
  *   k_scale, v_scale   float32 [heads], both or neither; only with KV_E4M3, where a stored value x stands for x * scale (NULL: scales
  *                      of 1).  Finite and > 0.
  *   page_size          tokens per page: a power of two, 16 ... 4096.    d: 64 or 128.

@@ -62,6 +62,40 @@ int check_rows(const void* p, const Dim* dims, int n, int d, int es, bool shared
     return KV_OK;
 }
 
+// Whether rows of d elements, `dims` of them from one address, meet the same rows from an address `diff` elements on.  Dimension by dimension from the longest stride: two rows
+// can only meet where their distance is no longer than what lies inside that stride.  (Strides that do not step over what lies inside them: taken to meet.)
+bool rows_meet(const Dim* dims, int n, i64 d, i64 diff)
+{
+    const Dim* by[4];
+    int count = 0;
+    for (int i = 0; i < n; ++i)
+        if (dims[i].size > 1) by[count++] = &dims[i];
+    for (int i = 1; i < count; ++i)
+        for (int k = i; k > 0 && by[k - 1]->stride < by[k]->stride; --k) { const Dim* const t = by[k]; by[k] = by[k - 1]; by[k - 1] = t; }
+    i64 inside[4], reach = d - 1;               // between the first element and the last of what lies inside a stride
+    for (int i = count - 1; i >= 0; --i) {
+        inside[i] = reach;
+        if (by[i]->stride <= reach) return true;
+        reach += (by[i]->size - 1) * by[i]->stride;
+    }
+    i64 left[16] = {diff};                      // distances that are left: at most two for each one before
+    int lefts = 1;
+    for (int i = 0; i < count; ++i) {
+        i64 next[16];
+        int nexts = 0;
+        for (int k = 0; k < lefts; ++k) {
+            const i64 s = by[i]->stride, low = left[k] / s - (left[k] % s < 0);
+            for (i64 step = low; step <= low + 1; ++step)
+                if (step > -by[i]->size && step < by[i]->size && left[k] - step * s <= inside[i] && step * s - left[k] <= inside[i]) next[nexts++] = left[k] - step * s;
+        }
+        for (int k = 0; k < nexts; ++k) left[k] = next[k];
+        lefts = nexts;
+    }
+    for (int k = 0; k < lefts; ++k)
+        if (left[k] < d && left[k] > -d) return true;
+    return false;
+}
+
 bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<std::uintptr_t>(p) & (to - 1)) != 0; }
 bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 int log2_of(int x) { int n = 0; while (x > 1) { x /= 2; ++n; } return n; }
@@ -88,6 +122,30 @@ int check_cache(const kv_pages* c, bool all_layers, bool scales, Extent* e)
     if (c->token_stride * c->page_size * es >= (1ll << 31)) return KV_ERR_OVERFLOW;
     if (c->k == c->v) return KV_ERR_ALIAS;
     return KV_OK;
+}
+
+// A cache that is written: keys and values must not meet.
+bool cache_meets(const kv_pages* c, bool all_layers, const Extent* e)
+{
+    if (!overlaps(e[0], e[1])) return false;
+    const int es = c->dtype == KV_E4M3 ? 1 : 2;
+    const Dim dims[4] = {{all_layers ? c->layers : 1, c->layer_stride}, {c->pages, c->page_stride}, {c->heads, c->head_stride}, {c->page_size, c->token_stride}};
+    return rows_meet(dims, 4, c->d, ((i64)e[1].first - (i64)e[0].first) / es);   // (both are multiples of 16 bytes)
+}
+
+// What a call reads beside its rows: the batch's arrays, the scales of the cache, frequencies.
+int side_inputs(const kv_pages* c, const kv_batch* b, const double* freq, int rot, Extent* e)
+{
+    e[0] = flat(b->q_start, 4ll * (b->sequences + 1ll));
+    e[1] = flat(b->kv_len, 4ll * b->sequences);
+    e[2] = flat(b->table, ((b->sequences - 1ll) * b->table_stride + b->table_width) * 4);
+    int n = 3;
+    if (c->k_scale) {
+        e[n++] = flat(c->k_scale, 4ll * c->heads);
+        e[n++] = flat(c->v_scale, 4ll * c->heads);
+    }
+    if (freq) e[n++] = flat(freq, rot / 2 * 8ll);
+    return n;
 }
 
 int check_batch(const kv_batch* b, const kv_pages* c)
@@ -156,6 +214,12 @@ bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads
     return fits((i64)p.splits * p.row_tiles, b->sequences) && fits(p.chunk_tiles, 1) && fits((i64)b->sequences * p.row_tiles, p.rows);
 }
 
+void book_arrays(const kv_book* b, Extent* e)
+{
+    e[0] = flat(b->table, ((i64)(b->rows - 1) * (b->rows > 1 ? b->table_stride : 0) + b->table_width) * 4);
+    e[1] = flat(b->ref, 4ll * b->pages);
+    e[2] = flat(b->kv_len, 4ll * b->rows);
+}
 int check_book(const kv_book* b)
 {
     if (!b) return KV_ERR_NULL;
@@ -164,22 +228,24 @@ int check_book(const kv_book* b)
     if (b->rows > 1 && b->table_stride < b->table_width) return KV_ERR_STRIDE;
     if (misaligned(b->ref, 4) || misaligned(b->table, 4) || misaligned(b->kv_len, 4)) return KV_ERR_ALIGN;
     if (b->pages > (1 << 28) || (i64)b->table_width * b->page_size >= (1ll << 31) || (i64)b->rows * b->table_stride >= (1ll << 46)) return KV_ERR_OVERFLOW;
-    const Extent t = flat(b->table, ((i64)(b->rows - 1) * (b->rows > 1 ? b->table_stride : 0) + b->table_width) * 4);
-    const Extent r = flat(b->ref, 4ll * b->pages), l = flat(b->kv_len, 4ll * b->rows);
-    if (overlaps(t, r) || overlaps(t, l) || overlaps(r, l)) return KV_ERR_ALIAS;
+    Extent e[3];
+    book_arrays(b, e);
+    if (overlaps(e[0], e[1]) || overlaps(e[0], e[2]) || overlaps(e[1], e[2])) return KV_ERR_ALIAS;
     return KV_OK;
 }
+// Whether something of so many ints overlaps one of the arrays.
+bool ints_overlap(const int* p, i64 n, const Extent* e, int count) { return n > 0 && overlaps_any(flat(p, 4 * n), e, count); }
 int check_list(const int* list, int n)
 {
     if (n < 0 || n > KV_MAX_LIST) return KV_ERR_SHAPE;
     if (n > 0 && !list) return KV_ERR_NULL;
     return misaligned(list, 4) ? KV_ERR_ALIGN : KV_OK;
 }
-int check_copy(const kv_pages* c)
+int check_copy(const kv_pages* c, Extent* e)
 {
-    Extent e[2];
     const int rc = check_cache(c, true, false, e);
     if (rc != KV_OK) return rc;
+    if (cache_meets(c, true, e)) return KV_ERR_ALIAS;
     return (i64)c->layers * 2 * ((i64)c->heads * c->page_size * c->d / 16384 + 1) >= (1ll << 23) ? KV_ERR_OVERFLOW : KV_OK;
 }
 PageCopy copy_of(const kv_pages* c)
@@ -222,6 +288,9 @@ int attn_paged_check_args(const kv_pages* cache, const kv_batch* batch, const kv
     const Extent el = flat(lse, 4ll * batch->tokens * heads), ew = flat(workspace, need);
     if (lse && (overlaps(el, eo) || overlaps_any(el, in, 3))) return KV_ERR_ALIAS;
     if (need > 0 && (overlaps(ew, eo) || overlaps_any(ew, in, 3) || (lse && overlaps(ew, el)))) return KV_ERR_ALIAS;
+    Extent side[6];
+    const int sides = side_inputs(cache, batch, nullptr, 0, side);
+    if (overlaps_any(eo, side, sides) || (lse && overlaps_any(el, side, sides)) || (need > 0 && overlaps_any(ew, side, sides))) return KV_ERR_ALIAS;
     return KV_OK;
 }
 
@@ -391,6 +460,11 @@ int kv_append_check_args(const kv_pages* cache, const kv_batch* batch, const kv_
             if (overlaps(out[2], in[i]) && !interleaved(q_out, heads, kv[i], cache->heads, cache->d)) return KV_ERR_ALIAS;
     }
     if (has_q && (overlaps(out[2], out[0]) || overlaps(out[2], out[1]))) return KV_ERR_ALIAS;
+    Extent side[6];
+    const int sides = side_inputs(cache, batch, freq, rot, side);
+    for (int i = 0; i < (has_q ? 3 : 2); ++i)
+        if (overlaps_any(out[i], side, sides)) return KV_ERR_ALIAS;
+    if (cache_meets(cache, false, out)) return KV_ERR_ALIAS;
     return KV_OK;
 }
 
@@ -451,6 +525,12 @@ int kv_reserve(const kv_book* book, const int* list, const int* new_len, int n, 
     if (!missing) return KV_ERR_NULL;
     if (misaligned(missing, 4)) return KV_ERR_ALIGN;
     if ((i64)n * book->table_width >= (1ll << 31)) return KV_ERR_OVERFLOW;       // (wants are counted in 32 bits)
+    Extent e[5];
+    book_arrays(book, e);
+    if (ints_overlap(list, n, e, 3) || ints_overlap(new_len, n, e, 3)) return KV_ERR_ALIAS;
+    e[3] = flat(list, 4ll * n);
+    e[4] = flat(new_len, 4ll * n);
+    if (ints_overlap(missing, 1, e, n > 0 ? 5 : 3)) return KV_ERR_ALIAS;
     return launched(kv_reserve_launch(*book, list, new_len, n, missing, stream));
 }
 
@@ -459,17 +539,26 @@ int kv_free(const kv_book* book, const int* list, int n, void* stream)
     int rc = check_book(book);
     if (rc != KV_OK) return rc;
     if ((rc = check_list(list, n)) != KV_OK) return rc;
+    Extent e[3];
+    book_arrays(book, e);
+    if (ints_overlap(list, n, e, 3)) return KV_ERR_ALIAS;
     return n == 0 ? KV_OK : launched(kv_free_launch(*book, list, n, stream));
 }
 
 int kv_fork(const kv_pages* cache, const kv_book* book, const int* src, const int* dst, int n, int* missing, void* stream)
 {
-    int rc = check_copy(cache);
+    Extent e[7];                                // the book, the cache, the lists
+    int rc = check_copy(cache, e + 3);
     if (rc != KV_OK || (rc = check_book(book)) != KV_OK) return rc;
     if ((rc = check_list(src, n)) != KV_OK || (rc = check_list(dst, n)) != KV_OK) return rc;
     if (!missing) return KV_ERR_NULL;
     if (misaligned(missing, 4)) return KV_ERR_ALIGN;
     if (!same_pages(cache, book)) return KV_ERR_SHAPE;
+    book_arrays(book, e);
+    if (ints_overlap(src, n, e, 5) || ints_overlap(dst, n, e, 5) || overlaps_any(e[3], e, 3) || overlaps_any(e[4], e, 3)) return KV_ERR_ALIAS;
+    e[5] = flat(src, 4ll * n);
+    e[6] = flat(dst, 4ll * n);
+    if (ints_overlap(missing, 1, e, n > 0 ? 7 : 5)) return KV_ERR_ALIAS;
     return launched(kv_fork_launch(copy_of(cache), *book, src, dst, n, missing, stream));
 }
 
@@ -477,20 +566,25 @@ long long kv_compact_workspace(int pages) { return pages < 1 || pages > (1 << 28
 
 int kv_compact(const kv_pages* cache, const kv_book* book, void* workspace, long long workspace_bytes, void* stream)
 {
-    int rc = check_copy(cache);
+    Extent e[5];                                // the book, the cache
+    int rc = check_copy(cache, e + 3);
     if (rc != KV_OK || (rc = check_book(book)) != KV_OK) return rc;
     if (!workspace) return KV_ERR_NULL;
     if (misaligned(workspace, 16)) return KV_ERR_ALIGN;
     if (!same_pages(cache, book)) return KV_ERR_SHAPE;
     if (workspace_bytes < kv_compact_workspace(book->pages)) return KV_ERR_WORKSPACE;
+    book_arrays(book, e);
+    if (overlaps_any(flat(workspace, kv_compact_workspace(book->pages)), e, 5) || overlaps_any(e[3], e, 3) || overlaps_any(e[4], e, 3)) return KV_ERR_ALIAS;
     return launched(kv_compact_launch(copy_of(cache), *book, (int*)workspace, stream));
 }
 
 int kv_copy_pages(const kv_pages* cache, const int* src, const int* dst, int n, void* stream)
 {
-    int rc = check_copy(cache);
+    Extent e[2];
+    int rc = check_copy(cache, e);
     if (rc != KV_OK) return rc;
     if ((rc = check_list(src, n)) != KV_OK || (rc = check_list(dst, n)) != KV_OK) return rc;
+    if (ints_overlap(src, n, e, 2) || ints_overlap(dst, n, e, 2)) return KV_ERR_ALIAS;
     return n == 0 ? KV_OK : launched(kv_copy_pages_launch(copy_of(cache), src, dst, n, stream));
 }
 

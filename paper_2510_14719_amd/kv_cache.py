@@ -215,6 +215,8 @@ def kv_append(k, v, k_cache, v_cache, q_start, kv_len, table, max_q, max_kv, q=N
     rc = _fast().kv_append(k, v, k_cache, v_cache, q_start, kv_len, table, max_q, max_kv, q, q_out, freq, layout, amplitude, k_scale, v_scale, stream)
     if rc is not NotImplemented:
         return _check(rc)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out: both or neither")
     tokens = k.shape[0]
     shape = (tokens, k_cache.shape[1], k_cache.shape[3])
     rk, rv = _rows(k, "k", shape, k.dtype), _rows(v, "v", shape, k.dtype)

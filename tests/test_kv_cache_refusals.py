@@ -48,6 +48,14 @@ def test_append_whose_outputs_overlap_what_it_reads(lib):
     assert f(o=freq + 256) == 0
 
 
+def test_queries_without_a_place_and_a_place_without_queries():
+    k, cache = torch.zeros((3, 2, 64), dtype=torch.float16), torch.zeros((5, 2, 16, 64), dtype=torch.float16)
+    ints, table = torch.zeros(4, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32)
+    for half in ({"q": k}, {"q_out": k}):
+        with pytest.raises(ValueError, match="both or neither"):
+            kv.kv_append(k, k, cache, cache, ints, ints[:3], table, 1, 1, **half)
+
+
 def meets(c, lib):
     """kv_copy_pages of nothing: only the cache is looked at."""
     return lib.kv_copy_pages(c, None, None, 0, None)

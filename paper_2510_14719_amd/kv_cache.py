@@ -102,6 +102,13 @@ def _fast():
     return binding._fast or binding._load_fast()
 
 
+def _int(x):
+    """A number for an int of the C ABI, which ctypes would cut to its lower 32 bits."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise KvCacheError(-5, _load().kv_strerror(-5).decode())
+    return x
+
+
 def _array(x, dtype, what, shape=None):
     """Address of a contiguous tensor of a type (and shape); None passes."""
     if x is None:
@@ -128,18 +135,18 @@ def _pages(k, v, k_scale=None, v_scale=None, layers=False):
         raise ValueError("k and v caches: two tensors of one type, shape and strides, %s[pages][heads][page size][d]; got %s and %s" % (
             "[layers]" if layers else "", tuple(k.shape), tuple(v.shape)))
     _unit(k, "cache")
-    n, h, t, d = k.shape[-4:]
+    n, h, t, d = map(_int, k.shape[-4:])
     s = k.stride()
     return _Pages(_device(k, "k cache"), _device(v, "v cache"), _array(k_scale, torch.float32, "k_scale", (h,)), _array(v_scale, torch.float32, "v_scale", (h,)),
-                  s[0] if layers else 0, s[-4], s[-3], s[-2], k.shape[0] if layers else 1, n, h, t, d, _type(k, "cache"))
+                  s[0] if layers else 0, s[-4], s[-3], s[-2], _int(k.shape[0]) if layers else 1, n, h, t, d, _type(k, "cache"))
 
 
 def _batch(q_start, kv_len, table, tokens, max_q, max_kv):
-    n = kv_len.shape[0]
+    n, tokens, max_q, max_kv = map(_int, (kv_len.shape[0], tokens, max_q, max_kv))
     if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != n or (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError("table: int32 [sequences][entries], entries contiguous; got %s %s" % (table.dtype, tuple(table.shape)))
-    return _Batch(_array(q_start, torch.int32, "q_start", (n + 1,)), _array(kv_len, torch.int32, "kv_len", (n,)), _device(table, "table"), n, tokens, table.shape[1],
-                  table.stride(0), max_q, max_kv)
+    return _Batch(_array(q_start, torch.int32, "q_start", (n + 1,)), _array(kv_len, torch.int32, "kv_len", (n,)), _device(table, "table"), n, tokens, _int(table.shape[1]),
+                  _int(table.stride(0)) if n > 1 else 0, max_q, max_kv)
 
 
 def _rows(x, what, shape=None, dtype=None):
@@ -155,8 +162,9 @@ def _stream(stream):
 
 def attn_paged_workspace(q, k_cache, sequences, max_q, max_kv) -> int:
     """Bytes of workspace of a call of ``attn_paged`` with these tokens, this cache (k or v) and these bounds."""
-    cache = _Pages(heads=k_cache.shape[1], d=k_cache.shape[3], dtype=_type(k_cache, "cache"))
-    n = _load().attn_paged_workspace(cache, _Batch(sequences=sequences, tokens=q.shape[0], max_q=max_q, max_kv=max_kv), q.shape[1])
+    cache = _Pages(heads=_int(k_cache.shape[1]), d=_int(k_cache.shape[3]), dtype=_type(k_cache, "cache"))
+    sequences, tokens, max_q, max_kv = map(_int, (sequences, q.shape[0], max_q, max_kv))
+    n = _load().attn_paged_workspace(cache, _Batch(sequences=sequences, tokens=tokens, max_q=max_q, max_kv=max_kv), _int(q.shape[1]))
     if n < 0:
         raise KvCacheError(-2, "no call takes these sizes")
     return n
@@ -176,14 +184,15 @@ def attn_paged(q, k_cache, v_cache, q_start, kv_len, table, o, lse, max_q, max_k
     if d != k_cache.shape[-1]:
         raise ValueError("q has heads of %d elements, the cache of %d" % (d, k_cache.shape[-1]))
     _check(_load().attn_paged(_pages(k_cache, v_cache, k_scale, v_scale), _batch(q_start, kv_len, table, tokens, max_q, max_kv), rq, ro,
-                              _array(lse, torch.float32, "lse", (tokens, heads)), heads, scale, int(bool(causal)), _type(q, "q"),
+                              _array(lse, torch.float32, "lse", (tokens, heads)), _int(heads), scale, int(bool(causal)), _type(q, "q"),
                               _array(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream(stream)))
 
 
 def rope_frequencies(rot, base=10000.0, scaling=PLAIN, factor=1.0, trained=0.0, low=1.0, high=32.0) -> torch.Tensor:
     """Radians per position of each pair, float64 [rot / 2] on the CPU: as they are, or for a context ``factor`` times the trained one (LINEAR: positions
     squeezed; BASE: a larger base; PARTS: pair by pair, by the turns that it makes in ``trained`` positions)."""
-    freq = (_cd * max(1, rot // 2))()
+    freq = (_cd * max(1, min(rot, 1024) // 2))()              # (more is refused)
+    rot = _int(rot)
     _check(_load().rope_frequencies(freq, rot, base, scaling, factor, trained, low, high))
     return torch.tensor(list(freq), dtype=torch.float64)
 
@@ -200,12 +209,12 @@ def rope(x, y, freq, pos=None, layout=HALF, amplitude=1.0, inverse=False, stream
         raise ValueError("x and y: two tensors of one type and shape [batch][heads][tokens][d]; got %s and %s" % (tuple(x.shape), tuple(y.shape)))
     _unit(x, "x")
     _unit(y, "y")
-    b, h, n, d = x.shape
+    b, h, n, d = map(_int, x.shape)
     if pos is not None and tuple(pos.shape) not in ((b, n), (n,)):
         raise ValueError("pos: [batch][tokens] or [tokens]; got %s" % (tuple(pos.shape),))
     stride = n if pos is not None and pos.dim() == 2 else 0
     _check(_load().rope(_Tensor(_device(x, "x"), *x.stride()[:3]), _Tensor(_device(y, "y"), *y.stride()[:3]), b, h, n, d, _array(pos, torch.int32, "pos"), stride,
-                        _array(freq, torch.float64, "freq"), 2 * freq.numel(), layout, amplitude, int(bool(inverse)), _type(x, "x"), _stream(stream)))
+                        _array(freq, torch.float64, "freq"), _int(2 * freq.numel()), _int(layout), amplitude, int(bool(inverse)), _type(x, "x"), _stream(stream)))
 
 
 def kv_append(k, v, k_cache, v_cache, q_start, kv_len, table, max_q, max_kv, q=None, q_out=None, freq=None, layout=HALF, amplitude=1.0, k_scale=None,
@@ -224,19 +233,21 @@ def kv_append(k, v, k_cache, v_cache, q_start, kv_len, table, max_q, max_kv, q=N
     if q is not None:
         rq, ro = _rows(q, "q", (tokens, q.shape[1], shape[2]), k.dtype), _rows(q_out, "q_out", tuple(q.shape), k.dtype)
     _check(_load().kv_append(_pages(k_cache, v_cache, k_scale, v_scale), _batch(q_start, kv_len, table, tokens, max_q, max_kv), rk, rv, rq, ro,
-                             0 if q is None else q.shape[1], _array(freq, torch.float64, "freq"), 0 if freq is None else 2 * freq.numel(), layout, amplitude,
+                             0 if q is None else _int(q.shape[1]), _array(freq, torch.float64, "freq"), 0 if freq is None else _int(2 * freq.numel()), _int(layout),
+                             amplitude,
                              _type(k, "k"), _stream(stream)))
 
 
 def _book(ref, table, kv_len, page_size):
-    rows = kv_len.shape[0]
+    rows = _int(kv_len.shape[0])
     if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != rows or (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError("table: int32 [rows][entries], entries contiguous; got %s %s" % (table.dtype, tuple(table.shape)))
-    return _Book(_array(ref, torch.int32, "ref"), _device(table, "table"), _array(kv_len, torch.int32, "kv_len"), ref.numel(), rows, table.shape[1], table.stride(0),
-                 page_size)
+    return _Book(_array(ref, torch.int32, "ref"), _device(table, "table"), _array(kv_len, torch.int32, "kv_len"), _int(ref.numel()), rows, _int(table.shape[1]),
+                 _int(table.stride(0)) if rows > 1 else 0, _int(page_size))
 
 
 def _list(x, n, what):
+    _int(n)
     return _array(x, torch.int32, what, (n,))
 
 
@@ -274,7 +285,7 @@ def kv_fork(k_cache, v_cache, ref, table, kv_len, src, dst, missing, stream=None
 
 def kv_compact_workspace(pages) -> int:
     """Bytes of workspace of ``kv_compact`` for a cache of so many pages."""
-    return _load().kv_compact_workspace(pages)
+    return _load().kv_compact_workspace(_int(pages))
 
 
 def kv_compact(k_cache, v_cache, ref, table, kv_len, workspace, stream=None) -> None:

@@ -291,3 +291,19 @@ def test_a_row_with_missing_pages_is_taken_up_again(kv):
     kv.kv_reserve(*m.dev, ints([2]), ints([70]), m.missing, 16)
     m.check("taken up", 1)
     assert m.table[2][:5] == [5, 0, 1, 2, -1] and m.ref == [1] * 6
+
+
+def test_numbers_beyond_an_int(kv):
+    b = Batch([(2, 40), (1, 9)], 4, 2, 64, "fp16", "fp16", 16)
+    dev = b.cuda()
+    big = 2 ** 32
+    args = (dev["q_start"], dev["kv_len"], dev["table"])
+    x = dev["q"].transpose(0, 1)[None]
+    freq = kv.rope_frequencies(64).cuda()
+    for call in (lambda: kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], *args, dev["o"], None, big + 2, 40, 1 / 8),
+                 lambda: kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], *args, dev["o"], None, 2, big + 40, 1 / 8),
+                 lambda: kv.kv_append(dev["q"][:, :2], dev["q"][:, :2], dev["k_cache"], dev["v_cache"], *args, big + 2, 40), lambda: kv.rope(x, torch.empty_like(x), freq, layout=big + 1),
+                 lambda: kv.kv_free(torch.zeros(5, dtype=torch.int32, device="cuda"), dev["table"], dev["kv_len"], ints([0]), big + 16)):
+        with pytest.raises(kv.KvCacheError) as e:
+            call()
+        assert e.value.code == -5

@@ -56,6 +56,19 @@ def test_queries_without_a_place_and_a_place_without_queries():
             kv.kv_append(k, k, cache, cache, ints, ints[:3], table, 1, 1, **half)
 
 
+def test_numbers_beyond_an_int():
+    """Not cut to their lower 32 bits, which would be another call's."""
+    q, cache = torch.zeros((3, 2, 64), dtype=torch.float16), torch.zeros((5, 2, 16, 64), dtype=torch.float16)
+    ints, table = torch.zeros(4, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32)
+    big = 2 ** 32
+    for call in (lambda: kv.attn_paged_workspace(q, cache, big + 1, 1, 32), lambda: kv.attn_paged_workspace(q, cache, 1, big + 1, 32), lambda: kv.attn_paged_workspace(q, cache, 1, 1, big + 32),
+                 lambda: kv.kv_compact_workspace(big + 5), lambda: kv.rope_frequencies(big + 64), lambda: kv._batch(ints, ints[:3], table, 3, big + 1, 32),
+                 lambda: kv._batch(ints, ints[:3], table, 3, 1, big + 32)):
+        with pytest.raises(kv.KvCacheError) as e:
+            call()
+        assert e.value.code == OVERFLOW
+
+
 def meets(c, lib):
     """kv_copy_pages of nothing: only the cache is looked at."""
     return lib.kv_copy_pages(c, None, None, 0, None)

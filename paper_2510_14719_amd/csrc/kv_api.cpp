@@ -211,7 +211,7 @@ bool grid_ok(const PagedPlan& p, const kv_pages* c, const kv_batch* b, int heads
 {
     const i64 most = 1ll << 23;                 // workgroups of 512 threads: a grid has less than 2^32
     auto fits = [&](i64 tiles, i64 splits) { return tiles < most && tiles * splits < most && tiles * splits * c->heads < most; };
-    return fits((i64)p.splits * p.row_tiles, b->sequences) && fits(p.chunk_tiles, 1) && fits((i64)b->sequences * p.row_tiles, p.rows);
+    return fits((i64)p.splits * p.row_tiles, b->sequences) && p.chunk_tiles < most && fits((i64)b->sequences * p.row_tiles, p.rows);
 }
 
 void book_arrays(const kv_book* b, Extent* e)

@@ -307,3 +307,23 @@ def test_numbers_beyond_an_int(kv):
         with pytest.raises(kv.KvCacheError) as e:
             call()
         assert e.value.code == -5
+
+
+def test_many_chunks_of_many_heads(kv):
+    """512 prompts of 1024 tokens, 64 heads: 131072 workgroups.  All read the same pages with the same Q, so all results are those of one prompt."""
+    S, N, H, d = 512, 1024, 64, 64
+    b = Batch([(N, N)], H, H, d, "bf16", "bf16", 64)
+    dev = b.cuda()
+    one, lse1 = torch.empty_like(dev["q"]), torch.empty((N, H), device="cuda")
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], one, lse1, N, N, 1 / 8,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], 1, N, N))
+    q, o, lse = dev["q"].repeat(S, 1, 1), torch.empty((S * N, H, d), dtype=torch.bfloat16, device="cuda"), torch.empty((S * N, H), device="cuda")
+    kv.attn_paged(q, dev["k_cache"], dev["v_cache"], torch.arange(S + 1, dtype=torch.int32, device="cuda") * N, dev["kv_len"].repeat(S), dev["table"].repeat(S, 1), o, lse, N, N, 1 / 8,
+                  workspace=workspace_for(kv, q, dev["k_cache"], S, N, N))
+    del q
+    o, lse = o.view(S, N * H * d), lse.view(S, N * H)
+    for s in range(1, S):
+        assert torch.equal(o[s], o[0]) and torch.equal(lse[s], lse[0]), s
+    # (another cut along the keys: both round the weights, 2 u of values up to 6 each, and the result)
+    assert float((o[0].float() - one.flatten().float()).abs().max()) <= 2 * 2 * 2.0 ** -8 * 6 and float((lse[0] - lse1.flatten()).abs().max()) <= 1e-4
+    assert bool(o[0].isfinite().all())

@@ -114,3 +114,13 @@ def test_books_that_overlap_what_is_read_or_written(lib):
         assert lib.kv_copy_pages(small, inside, L, 2, None) == lib.kv_copy_pages(small, L, inside, 2, None) == ALIAS
     assert lib.kv_compact(small, b, V, 1 << 20, None) == ALIAS
     assert lib.kv_reserve(b, L, L + 8, 2, L + 4, None) == lib.kv_fork(small, b, L, L + 8, 2, L + 12, None) == ALIAS       # `missing` in a list
+
+
+def test_many_chunks_fit_a_grid(lib):
+    """4194304 tokens of 64 heads on 16: 65536 chunks of each of 16 key heads, 2^20 workgroups of the 2^23 that there may be."""
+    b = batch(sequences=64, tokens=1 << 22, max_q=1 << 16, max_kv=1 << 16, table_width=4096, table_stride=4096)
+    wide = dict(token_stride=64 * 64)
+    assert lib.attn_paged_check_args(pages(heads=16, pages=1 << 18), b, rows(1 << 42, 64, **wide), rows(1 << 43, 64, **wide), None, 64, 0.125, 0, 1 << 44, 1 << 40) == 0
+    far = dict(heads=16, pages=1 << 18)
+    b = batch(sequences=64, tokens=1 << 25, max_q=1 << 20, max_kv=1 << 16, table_width=4096, table_stride=4096)
+    assert lib.attn_paged_check_args(pages(**far), b, rows(1 << 42, 64, **wide), rows(1 << 43, 64, **wide), None, 64, 0.125, 0, 1 << 44, 1 << 40) == OVERFLOW

@@ -134,10 +134,16 @@ void rope_kernel(RopeArgs a, int log_tokens, int head_step)
 
 // Eight values divided by the scale as E4M3: to nearest even, beyond the largest finite value to that one, NaN stays.  The quotient is x times the
 // reciprocal and one correction by the remainder, which rounds it as a division does (a division costs four times as much); far beyond 448, where the
-// correction might overflow, it does not matter.
-__device__ __forceinline__ u32x2 to_e4m3(const float (&x)[8], float scale, float reciprocal)
+// correction might overflow, it does not matter.  (A scale below the normal numbers may have no reciprocal: the values of such a head are brought up with it first.)
+__device__ __forceinline__ u32x2 to_e4m3(float (&x)[8], float scale, float reciprocal)
 {
     float v[8];
+    if (__builtin_expect(scale < 0x1p-126f, 0)) {
+        scale *= 0x1p64f;
+        reciprocal = 1.f / scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= 0x1p64f;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float q = x[i] * reciprocal, exact = __builtin_fmaf(__builtin_fmaf(-q, scale, x[i]), reciprocal, q);

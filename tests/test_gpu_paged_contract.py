@@ -327,3 +327,22 @@ def test_many_chunks_of_many_heads(kv):
     # (another cut along the keys: both round the weights, 2 u of values up to 6 each, and the result)
     assert float((o[0].float() - one.flatten().float()).abs().max()) <= 2 * 2 * 2.0 ** -8 * 6 and float((lse[0] - lse1.flatten()).abs().max()) <= 1e-4
     assert bool(o[0].isfinite().all())
+
+
+def test_scales_below_the_normal_numbers(kv):
+    """Of an E4M3 cache: what is stored is the quotient all the same, zeros are zeros."""
+    b = Batch([(3, 40), (2, 9)], 4, 2, 64, "bf16", "e4m3", 16)
+    g = torch.Generator().manual_seed(6)
+    scale = torch.tensor([1e-39, 2.0 ** -130])
+    x = (torch.randn((b.tokens, 2, 64), generator=g) * 200 * scale[None, :, None]).bfloat16()                # (quotients in the range of E4M3)
+    x[0] = 0.0
+    x[1, :, ::2] = 1.0                          # (far beyond it)
+    dev = b.cuda()
+    kv.kv_append(x.cuda(), x.cuda(), dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], b.max_q, b.max_kv, k_scale=scale.cuda(), v_scale=scale.cuda())
+    want = (x.double() / scale.double()[None, :, None]).clamp(-448, 448).float().to(torch.float8_e4m3fn).view(torch.uint8)
+    for name in ("k_cache", "v_cache"):
+        got = dev[name].view(torch.uint8).cpu()
+        for s, (n, m) in enumerate(b.lens):
+            for i in range(n):
+                pos = m - n + i
+                assert torch.equal(got[int(b.table[s, pos // 16]), :, pos % 16], want[int(b.q_start[s]) + i]), (name, s, i)

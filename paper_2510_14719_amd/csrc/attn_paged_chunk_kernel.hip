@@ -103,7 +103,7 @@ void attn_paged_chunk(PagedArgs a)
     nt_w = __builtin_amdgcn_readfirstlane(nt_w);
     nt_full = __builtin_amdgcn_readfirstlane(nt_full);
 
-    const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
+    const float scale = score_scale(a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f)), c = scale * 1.4426950408889634f;
     const float m_none = c > 1.f ? -0x1.fffff0p127f / c : -__FLT_MAX__;  // (the most negative float whose scaled value is finite)
 
     // ---- copies.  A wave's pieces are rows of one 16-key block of the tile and one 128-byte group of a row.

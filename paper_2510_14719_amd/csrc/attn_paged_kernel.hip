@@ -97,7 +97,7 @@ void attn_paged_few(PagedArgs a)
     }
     const int first_last = a.causal ? seq.first + tile * ROWS / a.group : keys - 1;   // what the first row sees
 
-    const float scale = a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f), c = scale * 1.4426950408889634f;
+    const float scale = score_scale(a.scale * (C8 && a.k_scale ? a.k_scale[h] : 1.f)), c = scale * 1.4426950408889634f;
     // The reference before the first score: the most negative float whose scaled value is finite.  (-inf would make NaN of rows whose
     // first keys are hidden.)
     const float m_none = c > 1.f ? -0x1.fffff0p127f / c : -__FLT_MAX__;

@@ -284,6 +284,9 @@ __device__ inline ChunkPiece own_numbered(const PagedArgs& a, const OwnSeq& all,
     return {-1, 0, 0, 1, 0};
 }
 
+// What a score is multiplied by.  Not zero, where the product of the call's scale and the keys' may be: hidden scores are -infinity.
+__device__ __forceinline__ float score_scale(float product) { return product < 0x1p-126f ? 0x1p-126f : product; }
+
 // ---- the sums of a row's weights
 //
 // The product with V takes the weights rounded to the type of the tokens.  O is divided by the sum of the same rounded weights, so that it is a mean of rows of V and

@@ -346,3 +346,22 @@ def test_scales_below_the_normal_numbers(kv):
             for i in range(n):
                 pos = m - n + i
                 assert torch.equal(got[int(b.table[s, pos // 16]), :, pos % 16], want[int(b.q_start[s]) + i]), (name, s, i)
+
+
+@pytest.mark.parametrize("lens,H,Hk,d", [([(6, 200), (2, 5)], 4, 2, 64), ([(2100, 2100)], 16, 16, 128)])
+def test_scales_whose_product_is_zero(kv, lens, H, Hk, d):
+    """In float32; all keys that a row sees weigh the same, and the others nothing."""
+    b = Batch(lens, H, Hk, d, "bf16", "e4m3", 16)
+    dev = b.cuda()
+    dev["scales"] = {"k_scale": torch.full((Hk,), 1e-30, device="cuda"), "v_scale": torch.ones(Hk, device="cuda")}
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], dev["lse"], b.max_q, b.max_kv, 1e-30,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), b.max_q, b.max_kv), **dev["scales"])
+    for s, (n, m) in enumerate(lens):
+        t0 = int(b.q_start[s])
+        v = b.v[s].double()
+        count = torch.arange(m - n + 1, m + 1).double()
+        want = (v.cumsum(0)[m - n:] / count[:, None, None]).repeat_interleave(H // Hk, 1)
+        size = (v.abs().cumsum(0)[m - n:] / count[:, None, None]).repeat_interleave(H // Hk, 1)
+        got = dev["o"][t0:t0 + n].double().cpu()
+        assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + m * 2.0 ** -23 * size).all()
+        assert torch.allclose(dev["lse"][t0:t0 + n].double().cpu(), count.log()[:, None].expand(n, H), rtol=2.0 ** -21, atol=m * 2.0 ** -24)

@@ -365,3 +365,54 @@ def test_scales_whose_product_is_zero(kv, lens, H, Hk, d):
         got = dev["o"][t0:t0 + n].double().cpu()
         assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + m * 2.0 ** -23 * size).all()
         assert torch.allclose(dev["lse"][t0:t0 + n].double().cpu(), count.log()[:, None].expand(n, H), rtol=2.0 ** -21, atol=m * 2.0 ** -24)
+
+
+def guarded(like, fill):
+    """A tensor of the same kind, 64 rows of `fill` before and behind it, and all of them."""
+    whole = torch.full((like.shape[0] + 128, *like.shape[1:]), fill, dtype=like.dtype, device="cuda")
+    return whole[64:64 + like.shape[0]], whole
+
+
+# sequences, tokens, max_q, max_kv, heads, key heads, d: small tiles in pieces; pieces beside chunks; chunks in pieces; prompts
+GARBAGE = [(6, 20, 4, 3000, 4, 1, 64), (150, 700, 33, 1500, 4, 1, 64), (8, 512, 64, 4000, 16, 4, 128), (3, 4200, 1500, 1500, 8, 2, 128), (130, 5200, 40, 4600, 4, 4, 128)]
+
+
+@pytest.mark.parametrize("cache", ["fp16", "e4m3"])
+@pytest.mark.parametrize("S,T,max_q,max_kv,H,Hk,d", GARBAGE)
+def test_starts_and_lengths_that_make_no_sense_write_nothing_else(kv, S, T, max_q, max_kv, H, Hk, d, cache):
+    """Falling, overlapping and endless starts, lengths and pages of all kinds: what lies beside O, LSE, the workspace, Q and the cache is left, and so are the rows that
+    no sequence can have."""
+    pages, rng = 40, random.Random(S)
+    b = Batch([(1, 1)], H, Hk, d, "fp16", cache, 64)
+    shape = (pages, Hk, 64, d)
+    q = torch.randn((T, H, d), device="cuda").half()
+    width = -(-max_kv // 64)
+    strange = [0, 1, -1, T - 1, T, T + 5, 2 ** 31 - 1, -2 ** 31]
+    for turn in range(4):
+        caches = [guarded(torch.zeros(shape, device="cuda").to(b.cache_dtype) if cache == "fp16" else torch.zeros(shape, dtype=torch.uint8, device="cuda"), 57) for _ in "kv"]
+        for c, _ in caches:
+            c.fill_(1)
+        k_cache, v_cache = (c if cache == "fp16" else c.view(b.cache_dtype) for c, _ in caches)
+        o, o_all = guarded(q, 77.0)
+        lse, lse_all = guarded(torch.empty((T, H), device="cuda"), 1234.5)
+        starts = [rng.choice(strange) if rng.random() < 0.2 else rng.randint(0, T) for _ in range(S + 1)]
+        if turn == 3:
+            starts = sorted(s for s in starts)
+        lens = [rng.choice([0, 1, -5, max_kv, max_kv + 1, 2 ** 31 - 1, -2 ** 31]) if rng.random() < 0.3 else rng.randint(0, max_kv) for _ in range(S)]
+        table = torch.randint(-3, pages + 3, (S, width), dtype=torch.int32)
+        args = (ints(starts), ints(lens), table.cuda())
+        n = kv.attn_paged_workspace(q, k_cache, S, max_q, max_kv)
+        work, work_all = guarded(torch.empty(max(n, 16), dtype=torch.uint8, device="cuda"), 0xa5)
+        kv.attn_paged(q, k_cache, v_cache, *args, o, lse, max_q, max_kv, 1 / 8, turn != 1, workspace=work[:n] if n else None)
+        q_out, q_all = guarded(q, 55.0)
+        kv.kv_append(q[:, :Hk], q[:, :Hk], k_cache, v_cache, *args, max_q, max_kv, q=q, q_out=q_out, freq=kv.rope_frequencies(d).cuda())
+        torch.cuda.synchronize()
+        for whole, fill in ((o_all, 77.0), (lse_all, 1234.5), (work_all, 0xa5), (q_all, 55.0), (caches[0][1], 57), (caches[1][1], 57)):
+            assert bool((whole[:64] == fill).all()) and bool((whole[-64:] == fill).all())
+        owned = torch.zeros(T, dtype=torch.bool)
+        for s in range(S):
+            q0 = min(max(starts[s], 0), T)
+            q1 = min(max(starts[s + 1], q0), T)
+            owned[q0:min(q1, q0 + max_q)] = True
+        for x, fill in ((o, 77.0), (lse, 1234.5), (q_out, 55.0)):
+            assert bool((x[~owned.cuda()] == fill).all())

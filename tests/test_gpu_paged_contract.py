@@ -416,3 +416,40 @@ def test_starts_and_lengths_that_make_no_sense_write_nothing_else(kv, S, T, max_
             owned[q0:min(q1, q0 + max_q)] = True
         for x, fill in ((o, 77.0), (lse, 1234.5), (q_out, 55.0)):
             assert bool((x[~owned.cuda()] == fill).all())
+
+
+@pytest.mark.parametrize("lens", [[(1, 40), (2, 9), (1, 1300)], [(9, 700), (1, 30), (40, 90)]])
+@pytest.mark.parametrize("cache", ["fp16", "e4m3"])
+def test_more_heads_on_a_key_head_than_rows_of_a_chunk(kv, lens, cache):
+    b = Batch(lens, 300, 1, 64, "fp16", cache, 16, pad=1)
+    dev = b.cuda()
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], dev["lse"], b.max_q, b.max_kv, 1 / 8,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], len(lens), b.max_q, b.max_kv), **dev["scales"])
+    torch.cuda.synchronize()
+    check(dev["o"], dev["lse"], b.reference(1 / 8, True))
+
+
+def test_more_sequences_than_two_steps_of_a_search(kv):
+    """5000 sequences, some without new tokens: each token finds its own, and attention sees what was appended."""
+    g = torch.Generator().manual_seed(8)
+    n = torch.randint(0, 3, (5000,), generator=g)
+    lens = [(int(a), int(a) + i % 40) for i, a in enumerate(n)]
+    b = Batch(lens, 1, 1, 64, "fp16", "fp16", 16, pad=2)
+    dev = b.cuda()
+    k, v = (torch.zeros((b.tokens, 1, 64), dtype=torch.float16) for _ in "kv")
+    for s, (a, m) in enumerate(lens):
+        t0 = int(b.q_start[s])
+        k[t0:t0 + a], v[t0:t0 + a] = b.k[s][m - a:], b.v[s][m - a:]
+        for pos in range(m - a, m):             # (what append has to bring is not there yet)
+            for name in ("k_cache", "v_cache"):
+                getattr(b, name)[int(b.table[s, pos // 16]), :, pos % 16] = float("nan")
+    before = [dev["k_cache"].clone(), dev["v_cache"].clone()]
+    dev["k_cache"].copy_(b.k_cache)
+    dev["v_cache"].copy_(b.v_cache)
+    kv.kv_append(k.cuda(), v.cuda(), dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], 2, b.max_kv)
+    for name, x in zip(("k_cache", "v_cache"), before):
+        assert torch.equal(dev[name].view(torch.int16), x.view(torch.int16))
+    kv.attn_paged(dev["q"], dev["k_cache"], dev["v_cache"], dev["q_start"], dev["kv_len"], dev["table"], dev["o"], dev["lse"], 2, b.max_kv, 1 / 8,
+                  workspace=workspace_for(kv, dev["q"], dev["k_cache"], 5000, 2, b.max_kv))
+    torch.cuda.synchronize()
+    check(dev["o"], dev["lse"], b.reference(1 / 8, True))

@@ -183,7 +183,7 @@ void attn_paged_chunk(PagedArgs a)
         }
     };
     // An 8-bit cache: into registers a stage ahead, widened once and written to the LDS (widened by every wave as it reads, the same values take the vector ALU longer
-    // than the products take the matrix cores: 4096 new tokens of 16384, 32 heads on 8, d 128: 1015 us that way, 848 so).
+    // than the products take the matrix cores: 4096 new tokens of 16384, 32 heads on 8, d 128: 1015 us that way, 848 so, and 885 with the sums of the rounded weights).
     u32x4 raw_k, raw_v;
     auto fetch_stage = [&](int st) __attribute__((always_inline)) {
         advance(st);
@@ -501,8 +501,9 @@ int launch_as(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 }
 
 // Whether chunks are cut for the keys that they see themselves: prompts of a few sequences (finding out takes longer the more there are; 6 of up to 1040 tokens, 5 heads on 1, E4M3, d 64 25 us
-// without, 29 with) whose chunks differ and are fewer than the compute units (16 heads, d 128, us without / with: one prompt of 2048 48.7 / 43.3, of 4096, 8 heads 67.3 / 55.9, of 3000, 16 on 2
-// 78.4 / 67.0; two of 1326, 20 on 4, E4M3, d 64 68.7 / 71.4).
+// without, 29 with) whose chunks differ, the first seeing at least a quarter fewer keys than the last (each has 256 / group tokens more than the one before), and are fewer than the compute
+// units.  us without / with, 16-bit: one prompt of 2048, 16 heads, d 128 49.0 / 43.2, of 4096, 8 heads 71.3 / 59.0, of 3000, 16 on 2 81.6 / 70.3; two of 1326, 20 on 4, d 64 61.7 / 62.0 (the
+// gain is lost to the longer way of finding out; over E4M3 68.7 / 71.4, the most that it costs).
 template <int DTYPE, bool C8, int D>
 int launch(const PagedArgs& a, const PagedPlan& plan, hipStream_t stream)
 {

@@ -366,7 +366,7 @@ void attn_paged_join(PagedArgs a)
     for (int i = lane; i < n; i += 64) m = __builtin_fmaxf(m, part_ml[i * all * 4]);
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, i));
-    // (every part has a finite reference, so m is finite)
+    // (a part without a key has a finite reference; a score of +infinity makes the row NaN here as in a whole one)
     f32x4 x = f32x4(0.f);
     f32x2 l = f32x2(0.f);                       // of the weights, and of the rounded ones
 #pragma unroll 4
@@ -486,8 +486,8 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
     p.split = whole;
     // Small tiles of 16 or 32 rows, or chunks of 256.  The former have many workgroups, fit for short calls, the latter feed the matrix cores better.  In keys that the places
     // of the chip walk through one after the other: chunks of sequences that they are cut for (or are not) cost as much as 400 (900) keys more.  us chunks / small tiles, d 128, 16-bit,
-    // 16 heads, one prompt of 64 8.3 / 5.7, 256 15.5 / 6.9, 512 20.8 / 12.1, 1024 29.5 / 25.2; 32 heads on 8, 64 tokens of 1000 21.0 / 12.8, 256 of 4000 35.2 / 51.8,
-    // one prompt of 1024 37.5 / 47.3.  Over 432 calls of all four kinds 23 % less on the mean than chunks for all with more than 32 rows, at most 9 % more.
+    // 16 heads, one prompt of 64 8.3 / 5.9, 256 15.7 / 7.2, 512 21.4 / 12.6, 1024 26.4 / 25.5, 2048 42.4 / 71.5; 32 heads on 8, 64 tokens of 1000 20.4 / 12.9, 256 of 4000 35.8 / 54,
+    // one prompt of 1024 32.7 / 47.
     const long long key_bytes = 2ll * d * cache_bytes;
     auto workgroups = [&](int rows) { return (double)((most + rows - 1) / rows) * sequences * key_heads; };
     auto places = [&](int rows, int kv) {       // what the LDS and the registers hold on 256 compute units
@@ -498,6 +498,10 @@ PagedPlan paged_plan(int sequences, int tokens, int max_q, int max_kv, int heads
     const double small = workgroups(32), chip = places(16, 256);
     const double keys = max_q < max_kv ? max_kv - 0.5 * max_q : 0.5 * max_kv;        // of a row on the mean, as most calls are
     const bool all_small = most <= 32 || (small <= 256 + chip && small * keys / chip <= (max_kv > 1024 ? 400 : 900) + workgroups(256) * keys / 256);
+    // With chunks, sequences of up to 32 rows go by small tiles, in a kernel of their own, where a batch has many workgroups, else by a chunk each.  That kernel costs 10 ... 20 us beside the
+    // chunks' and saves what many or long single tokens take longer as chunks.  us chunks for all / both (sequences x key heads): 16 heads on 4, 7 tokens of 4000 beside a prompt of 4096
+    // 110 / 131 (32), 8 of 1000 ... 4000 beside 8 prompts of 64 29 / 45 (64), 28 of 300 ... 8000 beside 4 of 1024 148 / 83 (128); 32 heads on 8, 60 of 300 ... 4000 beside 4 of 512 125 / 128 (512),
+    // 12 of 300 ... 2000 beside 12 of 256 54 / 63 (192), 7 of 65536 beside one of 2048 1115 / 392 (64): the product tells them apart only roughly, the last two are on the wrong side of it.
     p.few_rows = all_small ? 1 << 30 : (long long)sequences * key_heads > 64 ? 32 : 0;
     // 16 rows where they have a place each (with the pieces of long sequences) or, with more rows, no more rounds than those of 32: a step of 128 keys takes 1.0 us with 16 rows, 1.5 with 32.
     const double parts = max_kv > 1024 ? max_kv / 512. : 1., rounds = parts * workgroups(16) / places(16, max_kv), rounds32 = parts * small / places(32, max_kv);

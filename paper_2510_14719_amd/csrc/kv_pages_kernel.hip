@@ -165,12 +165,13 @@ __device__ __forceinline__ void copy_page(const PageCopy& c, char* base, int lay
     }
 }
 
-// Whether row s has a last page that is not full and is there.  (Where it is not, the continuation has none either: a page given out in its place would show
-// what its last owner left in it.)
-__device__ __forceinline__ bool has_part(const kv_book& b, int s)
+// The last page of row s, of len tokens, if it is not full and is there, else -1.  (Where it is not there, the continuation has none either: a page given out in its
+// place would show what its last owner left in it.)
+__device__ __forceinline__ int part_page(const kv_book& b, int s, int len)
 {
-    const int len = tokens_of(b, b.kv_len[s]);
-    return len % b.page_size > 0 && (unsigned)b.table[(long long)s * b.table_stride + len / b.page_size] < (unsigned)b.pages;
+    if (len % b.page_size == 0) return -1;
+    const int page = b.table[(long long)s * b.table_stride + len / b.page_size];
+    return (unsigned)page < (unsigned)b.pages ? page : -1;
 }
 
 __global__ __launch_bounds__(PLAN)
@@ -179,7 +180,7 @@ void fork_plan_kernel(kv_book b, const int* src, const int* dst, int n, int* mis
     extern __shared__ int before[];
     sum_list(before, n, [&](int i) {
         const int s = src[i], d = dst[i];
-        return (unsigned)s < (unsigned)b.rows && (unsigned)d < (unsigned)b.rows && s != d && has_part(b, s) ? 1 : 0;
+        return (unsigned)s < (unsigned)b.rows && (unsigned)d < (unsigned)b.rows && s != d && part_page(b, s, tokens_of(b, b.kv_len[s])) >= 0 ? 1 : 0;
     });
     const int want = before[n];
     auto place = [&](int k) -> int& {
@@ -200,13 +201,12 @@ void fork_kernel(PageCopy c, kv_book b, const int* src, const int* dst, int part
 {
     const int s = src[blockIdx.y], d = dst[blockIdx.y];
     if ((unsigned)s >= (unsigned)b.rows || (unsigned)d >= (unsigned)b.rows || s == d) return;
-    const int len = tokens_of(b, b.kv_len[s]), full = len / b.page_size;
-    const bool part = has_part(b, s);
+    const int len = tokens_of(b, b.kv_len[s]), full = len / b.page_size, part = part_page(b, s, len);
     const int* const from = b.table + (long long)s * b.table_stride;
     int* const to = b.table + (long long)d * b.table_stride;
     if (blockIdx.x == 0) {
         for (int j = threadIdx.x; j < b.table_width; j += 256) {
-            if (j == full && part) continue;    // (the plan has put it there)
+            if (j == full && part >= 0) continue;    // (the plan has put it there)
             const int page = j < full ? from[j] : -1;
             to[j] = page;
             if ((unsigned)page < (unsigned)b.pages) atomicAdd(&b.ref[page], 1);
@@ -214,13 +214,13 @@ void fork_kernel(PageCopy c, kv_book b, const int* src, const int* dst, int part
         if (threadIdx.x == 0) b.kv_len[d] = len;
         return;
     }
-    if (!part) return;
-    const int old = from[full], now = to[full];
+    if (part < 0) return;
+    const int now = to[full];
     if ((unsigned)now >= (unsigned)b.pages) return;
     int id = blockIdx.x - 1;
     const int p = id % parts;
     id /= parts;
-    copy_page(c, id & 1 ? c.v : c.k, id >> 1, old, now, p, parts);
+    copy_page(c, id & 1 ? c.v : c.k, id >> 1, part, now, p, parts);
 }
 
 __global__ __launch_bounds__(256)
